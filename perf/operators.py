@@ -314,7 +314,7 @@ def _plain_write(st, k, v, past, count):
         if case["bits"] == 16:
             to[0][page, slot] = x.bfloat16()
             continue
-        x = x.clamp(-65504.0, 65504.0).reshape(B, T, Hk, d // GROUP, GROUP)
+        x = x.clamp(-65024.0, 65024.0).reshape(B, T, Hk, d // GROUP, GROUP)
         least = x.amin(-1)
         unit = ((x.amax(-1) - least) / 15.0).half()
         least = least.half()
@@ -481,7 +481,7 @@ def _exact_held(case, x):
     """The values that the cache holds for float64 rows [..., d]."""
     if case["bits"] == 16:
         return x.bfloat16().double()
-    g = x.clamp(-65504, 65504).unflatten(-1, (x.shape[-1] // GROUP, GROUP))
+    g = x.clamp(-65024, 65024).unflatten(-1, (x.shape[-1] // GROUP, GROUP))
     low, high = g.min(-1, keepdim=True).values, g.max(-1, keepdim=True).values
     unit, low = ((high - low) / 15).float().half().double(), low.float().half().double()
     code = torch.where(unit > 0, torch.round((g - low) / unit.clamp(min=1e-30)), 0.0).clamp(0, 15)
