@@ -209,6 +209,87 @@ pa_status power_attn_decode_step(const pa_problem* prob, const void* q, const vo
                                  const float* log_g, void* state, size_t state_bytes,
                                  void* o, float* z, void* hip_stream);
 
+/* ---- exponential attention -----------------------------------------------------------------------
+ * The weight that the paper compares power attention with (softmax attention, Sec. 2 Eq. (1)), on grouped heads and with the
+ * scores and masks that models use it with.  Query i of T stands at position pos_i = i + Tk - T among Tk keys; head h reads key
+ * head h / (H / Hk):
+ *     x_ij = scale q_i.k_j,   s_ij = cap tanh(x_ij / cap)  (cap > 0; x_ij without),   less slope_h |pos_i - j|  (slopes given)
+ *     L_i  = log sum_j exp(s_ij),   O_i = sum_j exp(s_ij - L_i) v_j   over the keys j that row i sees:
+ *            lo_i <= j < hi_i   and   j > pos_i - window  (window > 0)
+ * lo, hi: DEVICE int32 [B, T], the same for all heads, either may be NULL: lo = 0, hi = pos_i + 1 (causal).  Values are clamped to
+ * 0 .. Tk.  Packed documents: lo_i = the first token of i's document; a prefix that its whole document sees: hi_i = max(pos_i +
+ * 1, end of the prefix); padding: hi_i = lo_i; no causal mask: hi_i = Tk.  A row that sees no key gets O_i = 0, L_i = -infinity
+ * and passes no gradient.  What the rows and keys that a row does not see hold, infinities and NaN among it, does not reach it.
+ * bf16, d in {32, 64, 128}, T and Tk up to 2^30 tokens.  Q, O, dO, dQ [B, H, T, d], K, V, dK, dV [B, Hk, Tk, d], L float32
+ * [B, H, T], slopes float32 [H], not differentiated.  Pointers, streams, threads and errors as for the calls above, but that
+ * L, slopes, lo and hi need the alignment of their type only.  Results do not change from run to run. */
+typedef struct {
+    int   B, H, Hk;     /* batch, query heads, key heads (H a multiple of Hk) */
+    int   T, Tk, d;     /* queries, keys, head size */
+    float scale;        /* > 0 */
+    float cap;          /* > 0: scores are capped by cap tanh(x / cap); 0: they are not */
+    int   window;       /* > 0: only keys behind pos_i - window; 0: no window */
+    int   dtype;        /* pa_dtype */
+} pa_exp_problem;
+
+/* PA_OK if the calls below take `prob`; the bytes of device scratch that they need for it (0 also on an invalid problem). */
+pa_status power_attn_exp_supported(const pa_exp_problem* prob, int for_backward);
+size_t power_attn_exp_workspace_bytes(const pa_exp_problem* prob, int for_backward);
+
+/* L may be NULL when it is not wanted. */
+pa_status power_attn_exp_fwd(const pa_exp_problem* prob, const void* Q, const void* K, const void* V, const float* slopes,
+                             const int* row_lo, const int* row_hi, void* O, float* L,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+/* From the forward pass's O and L and dO: dQ, dK, dV (a key head's gradients are sums over the heads that read it). */
+pa_status power_attn_exp_bwd(const pa_exp_problem* prob, const void* Q, const void* K, const void* V, const float* slopes,
+                             const int* row_lo, const int* row_hi, const void* O, const float* L, const void* dO,
+                             void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- paged cache of keys and values ----------------------------------------------------------------
+ * What exponential attention decodes from, as the power attention's decode state is for it, but growing: tokens are held in
+ * pages of a pool that the caller owns, and sequence b finds position t in page table[b][t / page].  A pool holds all key heads
+ * of one layer in an order of its own, as bf16 or in 4 bits: per token, key head and 32 channels the minimum m and the unit
+ * u = (max - min) / 15 as fp16 and 32 codes c, x = u c + m.  (Computed from the values limited to +-65024, so that every x lies in
+ * the range of fp16, in float32; u and m rounded to nearest, c the nearest integer to (x - m) / u within 0 .. 15, ties to even; 0 where u is 0.  A group
+ * with a NaN in it reads back as NaN.)
+ * pool: DEVICE, power_attn_cache_bytes() bytes, 16-byte aligned, needs no initialisation.  table: DEVICE int32 [B, max_pages];
+ * lengths and positions: DEVICE int32 [B].  Nothing of them is read by the host, so a captured graph can be replayed with others
+ * in the same place.  A page index outside 0 .. num_pages - 1 stands for no page: nothing is written there, reads give zeros,
+ * and a step leaves its tokens out.  Two sequences may share pages that are only read.  d in {64, 128}.  Alignment: pool, K, V, Q, q, o, cos, sin 16 bytes, the other
+ * arrays that of their type.  Up to 65535 sequences and heads, 2^30 positions a sequence and 2^29 rows a call. */
+typedef struct {
+    int   B, H, Hk, d;              /* sequences, query heads, key heads (H a multiple of Hk), head size */
+    int   page;                     /* tokens per page: a power of two, 32 .. 1024 */
+    int   max_pages, num_pages;     /* columns of the table; pages of the pool */
+    int   bits;                     /* 16 or 4 */
+    int   rot;                      /* channels 0 .. rot - 1 are rotated: 0 or a multiple of 16 up to d */
+    int   rot_adjacent;             /* 0: channel c turns with c + rot / 2; 1: channel 2 c with 2 c + 1 */
+    int   rot_rows;                 /* rows of cos and sin, at least max_pages page where rot > 0 */
+    float scale, cap;               /* of a step's scores: as in pa_exp_problem */
+    int   window;
+} pa_cache;
+
+size_t power_attn_cache_bytes(const pa_cache* cache);       /* 0 on an invalid cache */
+
+/* Puts rows t = 0 .. count[b] - 1 of K, V [B, Hk, T, d] (bf16; count NULL: all T) at positions past[b] + t of sequence b, K rotated
+ * on the way: with the pair (x, y) of channels that angle number a turns, position t and c = cos[t][a], s = sin[t][a] (DEVICE
+ * float32 [rot_rows, rot / 2]) (x c - y s, y c + x s), in float32, rounded once.  Q (may be NULL) [B, H, T, d] is rotated
+ * likewise into Q_out, which may be Q itself.  K and V may both be NULL (only queries).  Rows with t >= count[b] or a position outside the
+ * table (t + past[b] < 0, >= max_pages page) are not written, in Q_out neither.  Sequences of one call must not write to one page. */
+pa_status power_attn_cache_append(const pa_cache* cache, int T, const void* K, const void* V, const void* Q, void* Q_out,
+                                  const float* cos, const float* sin, void* pool, const int* table, const int* past,
+                                  const int* count, void* hip_stream);
+/* K, V [B, Hk, T, d] (bf16) = the values held at positions start[b] + t, t < count[b] (NULL: all T).  The other rows and those
+ * outside the table are left as they are. */
+pa_status power_attn_cache_read(const pa_cache* cache, int T, const void* pool, const int* table, const int* start,
+                                const int* count, void* K, void* V, void* hip_stream);
+/* One token for every sequence: q [B, H, d] (rotated), the last of lens[b] tokens held, attends to them (pos = lens[b] - 1):
+ * o [B, H, d] and, where L is not NULL, L [B, H] as power_attn_exp_fwd has them.  lens[b] <= 0: o = 0, L = -infinity; lengths are
+ * limited to the table.  4 bits: the values enter the products as fp16.  workspace: DEVICE, 256-byte aligned. */
+size_t power_attn_cache_step_workspace_bytes(const pa_cache* cache);
+pa_status power_attn_cache_step(const pa_cache* cache, const void* q, const float* slopes, const void* pool, const int* table,
+                                const int* lens, void* o, float* L, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* The chunk size the calls use for `prob` (prob->chunk itself unless it is 0; 0 on an invalid problem).  Where the kernels space
  * their states themselves (see pa_problem.chunk and power_attn_state_spacing) it only says that the chunked form is asked for.  Un-gated float32
  * calls under PA_IMPL_AUTO with d = v in {16, 32, 64, 128} and T <= 4096 (<= 16384 where B H T <= 262144) run the attention

@@ -34,6 +34,15 @@ EXPORTED_SYMBOLS = (
     "power_attn_bwd",
     "power_attn_fwd_gated",
     "power_attn_bwd_gated",
+    "power_attn_exp_supported",
+    "power_attn_exp_workspace_bytes",
+    "power_attn_exp_fwd",
+    "power_attn_exp_bwd",
+    "power_attn_cache_bytes",
+    "power_attn_cache_append",
+    "power_attn_cache_read",
+    "power_attn_cache_step_workspace_bytes",
+    "power_attn_cache_step",
     "power_attn_state_rows",
     "power_attn_state_spacing",
     "power_attn_resolved_chunk",
@@ -54,6 +63,19 @@ class PaProblem(ctypes.Structure):
                 ("v", ctypes.c_int), ("p", ctypes.c_int), ("chunk", ctypes.c_int), ("normalize", ctypes.c_int),
                 ("scale", ctypes.c_float), ("dtype", ctypes.c_int), ("impl", ctypes.c_int),
                 ("keep_state", ctypes.c_int), ("gated", ctypes.c_int), ("d_tile", ctypes.c_int)]
+
+
+class PaExpProblem(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("Hk", ctypes.c_int), ("T", ctypes.c_int), ("Tk", ctypes.c_int),
+                ("d", ctypes.c_int), ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int),
+                ("dtype", ctypes.c_int)]
+
+
+class PaCache(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int), ("H", ctypes.c_int), ("Hk", ctypes.c_int), ("d", ctypes.c_int), ("page", ctypes.c_int),
+                ("max_pages", ctypes.c_int), ("num_pages", ctypes.c_int), ("bits", ctypes.c_int), ("rot", ctypes.c_int),
+                ("rot_adjacent", ctypes.c_int), ("rot_rows", ctypes.c_int), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("window", ctypes.c_int)]
 
 
 class PaKernelTime(ctypes.Structure):
@@ -115,6 +137,26 @@ def load_library():
     lib.power_attn_fwd_gated.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.power_attn_bwd_gated.restype = ctypes.c_int
     lib.power_attn_bwd_gated.argtypes = [P, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    E = ctypes.POINTER(PaExpProblem)
+    lib.power_attn_exp_supported.restype = ctypes.c_int
+    lib.power_attn_exp_supported.argtypes = [E, ctypes.c_int]
+    lib.power_attn_exp_workspace_bytes.restype = ctypes.c_size_t
+    lib.power_attn_exp_workspace_bytes.argtypes = [E, ctypes.c_int]
+    lib.power_attn_exp_fwd.restype = ctypes.c_int
+    lib.power_attn_exp_fwd.argtypes = [E, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.power_attn_exp_bwd.restype = ctypes.c_int
+    lib.power_attn_exp_bwd.argtypes = [E, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    C = ctypes.POINTER(PaCache)
+    lib.power_attn_cache_bytes.restype = ctypes.c_size_t
+    lib.power_attn_cache_bytes.argtypes = [C]
+    lib.power_attn_cache_append.restype = ctypes.c_int
+    lib.power_attn_cache_append.argtypes = [C, ctypes.c_int, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.power_attn_cache_read.restype = ctypes.c_int
+    lib.power_attn_cache_read.argtypes = [C, ctypes.c_int, vp, vp, vp, vp, vp, vp, vp]
+    lib.power_attn_cache_step_workspace_bytes.restype = ctypes.c_size_t
+    lib.power_attn_cache_step_workspace_bytes.argtypes = [C]
+    lib.power_attn_cache_step.restype = ctypes.c_int
+    lib.power_attn_cache_step.argtypes = [C, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.power_attn_status_string.restype = ctypes.c_char_p
     lib.power_attn_status_string.argtypes = [ctypes.c_int]
     lib.power_attn_last_hip_error.restype = ctypes.c_char_p
@@ -386,3 +428,201 @@ def power_attn_decode_step(prob: PaProblem, q, k, v, state, log_g=None, out=None
     if st != 0:
         _check(lib, st, "power_attn_decode_step")
     return o, z
+
+
+# ---- exponential attention ----
+def make_exp_problem(B, H, Hk, T, Tk, d, scale=1.0, cap=0.0, window=0, dtype="bf16") -> PaExpProblem:
+    return PaExpProblem(B, H, Hk, T, Tk, d, float(scale), float(cap), int(window), PA_DTYPE_BF16 if dtype == "bf16" else PA_DTYPE_F32)
+
+
+@functools.lru_cache(maxsize=512)
+def _exp_plan(for_backward, B, H, Hk, T, Tk, d, scale, cap, window, dtype):
+    """-> (pointer to the problem, power_attn_exp_supported's status, workspace bytes)"""
+    lib = load_library()
+    ref = ctypes.pointer(make_exp_problem(B, H, Hk, T, Tk, d, scale, cap, window, dtype))
+    return ref, int(lib.power_attn_exp_supported(ref, for_backward)), int(lib.power_attn_exp_workspace_bytes(ref, for_backward))
+
+
+def _exp_plan_of(for_backward, Q, K, V, scale, cap, window):
+    if Q.dim() != 4 or K.dim() != 4:
+        raise PowerAttnError("tensors must be [B, H, T, d]")
+    B, H, T, d = Q.shape
+    if K.shape[0] != B or K.shape[3] != d or K.shape != V.shape:
+        raise PowerAttnError("K and V must be [B, Hk, Tk, d] of Q's B and d")
+    return _exp_plan(for_backward, B, H, K.shape[1], T, K.shape[2], d, float(scale), float(cap), operator.index(window), _dtype_name(Q))
+
+
+def _array_ptr(t, like, shape, dtype, name):
+    """Device pointer of an optional contiguous array on `like`'s device"""
+    if t is None:
+        return None
+    if t.device != like.device or not t.is_contiguous() or t.dtype is not dtype or tuple(t.shape) != tuple(shape):
+        raise PowerAttnError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on the device of the others")
+    return t.data_ptr()
+
+
+def _shaped_ptr(t, like, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise PowerAttnError(f"{name} must be {list(shape)}")
+    return _dev_ptr(t, like, name)
+
+
+def power_attn_exp_supported(prob: PaExpProblem, for_backward: bool) -> bool:
+    return int(load_library().power_attn_exp_supported(ctypes.byref(prob), int(for_backward))) == 0
+
+
+def power_attn_exp_workspace_bytes(prob: PaExpProblem, for_backward: bool) -> int:
+    return int(load_library().power_attn_exp_workspace_bytes(ctypes.byref(prob), int(for_backward)))
+
+
+def _exp_masks(Q, slopes, row_lo, row_hi):
+    import torch
+    B, H, T, _ = Q.shape
+    return (_array_ptr(slopes, Q, (H,), torch.float32, "slopes"), _array_ptr(row_lo, Q, (B, T), torch.int32, "row_lo"),
+            _array_ptr(row_hi, Q, (B, T), torch.int32, "row_hi"))
+
+
+def power_attn_exp_fwd(Q, K, V, scale: float = 1.0, cap: float = 0.0, window: int = 0, slopes=None, row_lo=None, row_hi=None,
+                       workspace=None, out=None, out_lse=None):
+    """Exponential (softmax) attention on the current stream: Q [B, H, T, d], K, V [B, Hk, Tk, d] -> (O like Q, L float32 [B, H, T]).
+    cap > 0 caps the scores by cap tanh(x / cap); slopes (float32 [H]) subtracts slope |pos - j|; row i sees the keys row_lo[b, i]
+    <= j < row_hi[b, i] (int32 [B, T]; without them all up to its position i + Tk - T) of the last `window`, if one is given."""
+    import torch
+    lib = load_library()
+    q, k, v = _dev_ptr(Q, None, "Q"), _dev_ptr(K, Q, "K"), _dev_ptr(V, Q, "V")
+    prob, status, need = _exp_plan_of(0, Q, K, V, scale, cap, window)
+    if status != 0:
+        _check(lib, status, "power_attn_exp_fwd")
+    masks = _exp_masks(Q, slopes, row_lo, row_hi)
+    with _OnDevice(Q.device):
+        O = torch.empty_like(Q) if out is None else out
+        L = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if out_lse is None else out_lse
+        ws = 0
+        if need > 0:
+            workspace, ws = _workspace(need, workspace, Q.device)
+        st = lib.power_attn_exp_fwd(prob, q, k, v, *masks, _shaped_ptr(O, Q, Q.shape, "O"),
+                                    _array_ptr(L, Q, Q.shape[:3], torch.float32, "L"), ws, need, _stream())
+    if st != 0:
+        _check(lib, st, "power_attn_exp_fwd")
+    return O, L
+
+
+def power_attn_exp_bwd(Q, K, V, O, L, dO, scale: float = 1.0, cap: float = 0.0, window: int = 0, slopes=None, row_lo=None, row_hi=None,
+                       workspace=None, out=None):
+    """Backward pass of power_attn_exp_fwd on the current stream: its O and L, and dO -> (dQ, dK, dV)."""
+    import torch
+    lib = load_library()
+    q, k, v, g = _dev_ptr(Q, None, "Q"), _dev_ptr(K, Q, "K"), _dev_ptr(V, Q, "V"), _shaped_ptr(dO, Q, Q.shape, "dO")
+    prob, status, need = _exp_plan_of(1, Q, K, V, scale, cap, window)
+    if status != 0:
+        _check(lib, status, "power_attn_exp_bwd")
+    masks = _exp_masks(Q, slopes, row_lo, row_hi)
+    with _OnDevice(Q.device):
+        dQ, dK, dV = (torch.empty_like(x) for x in (Q, K, V)) if out is None else out
+        workspace, ws = _workspace(need, workspace, Q.device)
+        st = lib.power_attn_exp_bwd(prob, q, k, v, *masks, _shaped_ptr(O, Q, Q.shape, "O"), _array_ptr(L, Q, Q.shape[:3], torch.float32, "L"),
+                                    g, _shaped_ptr(dQ, Q, Q.shape, "dQ"), _shaped_ptr(dK, Q, K.shape, "dK"),
+                                    _shaped_ptr(dV, Q, K.shape, "dV"), ws, need, _stream())
+    if st != 0:
+        _check(lib, st, "power_attn_exp_bwd")
+    return dQ, dK, dV
+
+
+# ---- the paged cache that it decodes from ----
+def make_cache(B, H, Hk, d, page, max_pages, num_pages, bits=16, rot=0, rot_adjacent=False, rot_rows=0, scale=1.0, cap=0.0,
+               window=0) -> PaCache:
+    return PaCache(B, H, Hk, d, page, max_pages, num_pages, bits, rot, int(bool(rot_adjacent)), rot_rows, float(scale), float(cap), int(window))
+
+
+def power_attn_cache_bytes(cache: PaCache) -> int:
+    return int(load_library().power_attn_cache_bytes(ctypes.byref(cache)))
+
+
+def power_attn_cache_step_workspace_bytes(cache: PaCache) -> int:
+    return int(load_library().power_attn_cache_step_workspace_bytes(ctypes.byref(cache)))
+
+
+def _cache_ptrs(lib, cache, pool, table, what):
+    """Pointers of pool and table, which must be as large as the cache says"""
+    import torch
+    need = int(lib.power_attn_cache_bytes(ctypes.byref(cache)))
+    if need == 0:
+        raise PowerAttnError(f"{what}: invalid or unsupported cache")
+    if pool.numel() * pool.element_size() < need:
+        raise PowerAttnError(f"{what}: pool holds {pool.numel() * pool.element_size()} bytes, {need} needed")
+    return _dev_ptr(pool, name="pool"), _array_ptr(table, pool, (cache.B, cache.max_pages), torch.int32, "table")
+
+
+def _lengths_ptr(t, pool, cache, name):
+    import torch
+    return _array_ptr(t, pool, (cache.B,), torch.int32, name)
+
+
+def _rows_ptr(t, pool, cache, heads, T, name):
+    import torch
+    if t.dtype is not torch.bfloat16 or t.device != pool.device or tuple(t.shape) != (cache.B, heads, T, cache.d):
+        raise PowerAttnError(f"{name} must be bfloat16 {[cache.B, heads, T, cache.d]} on the pool's device")
+    return _dev_ptr(t, name=name)
+
+
+def power_attn_cache_append(cache: PaCache, K, V, pool, table, past, count=None, Q=None, cos=None, sin=None, out_q=None):
+    """K, V [B, Hk, T, d] (or None) into the cache at positions past[b] + t, t < count[b], keys rotated by cos, sin (float32
+    [rot_rows, rot / 2]) on the way; -> Q [B, H, T, d] rotated likewise, into out_q (which may be Q), or None without Q."""
+    import torch
+    lib = load_library()
+    if (K is None) != (V is None) or (K is None and Q is None):
+        raise PowerAttnError("power_attn_cache_append: K and V, Q, or all of them")
+    T = (K if K is not None else Q).shape[2]
+    with _OnDevice(pool.device):
+        p, t = _cache_ptrs(lib, cache, pool, table, "power_attn_cache_append")
+        k = v = q = qo = c = s = None
+        if K is not None:
+            k, v = _rows_ptr(K, pool, cache, cache.Hk, T, "K"), _rows_ptr(V, pool, cache, cache.Hk, T, "V")
+        if Q is not None:
+            q = _rows_ptr(Q, pool, cache, cache.H, T, "Q")
+            out_q = torch.empty_like(Q) if out_q is None else out_q
+            qo = _rows_ptr(out_q, pool, cache, cache.H, T, "out_q")
+        if cache.rot > 0:
+            shape = (cache.rot_rows, cache.rot // 2)
+            c, s = _array_ptr(cos, pool, shape, torch.float32, "cos"), _array_ptr(sin, pool, shape, torch.float32, "sin")
+        st = lib.power_attn_cache_append(cache, T, k, v, q, qo, c, s, p, t, _lengths_ptr(past, pool, cache, "past"),
+                                         _lengths_ptr(count, pool, cache, "count"), _stream())
+    if st != 0:
+        _check(lib, st, "power_attn_cache_append")
+    return out_q if Q is not None else None
+
+
+def power_attn_cache_read(cache: PaCache, pool, table, start, T: int, count=None, out=None):
+    """-> K, V [B, Hk, T, d] bfloat16: the values held at positions start[b] + t, t < count[b].  Rows that are not there are left as
+    they are in `out`, and undefined without it."""
+    import torch
+    lib = load_library()
+    with _OnDevice(pool.device):
+        p, t = _cache_ptrs(lib, cache, pool, table, "power_attn_cache_read")
+        K, V = out if out is not None else (torch.empty(cache.B, cache.Hk, T, cache.d, dtype=torch.bfloat16, device=pool.device)
+                                            for _ in range(2))
+        st = lib.power_attn_cache_read(cache, T, p, t, _lengths_ptr(start, pool, cache, "start"), _lengths_ptr(count, pool, cache, "count"),
+                                       _rows_ptr(K, pool, cache, cache.Hk, T, "K"), _rows_ptr(V, pool, cache, cache.Hk, T, "V"), _stream())
+    if st != 0:
+        _check(lib, st, "power_attn_cache_read")
+    return K, V
+
+
+def power_attn_cache_step(cache: PaCache, q, pool, table, lens, slopes=None, out=None, out_lse=None, workspace=None):
+    """One token for every sequence: q [B, H, d] (rotated), the last of the lens[b] tokens held -> (o [B, H, d], L [B, H] float32)."""
+    import torch
+    lib = load_library()
+    if q.dtype is not torch.bfloat16 or q.device != pool.device or tuple(q.shape) != (cache.B, cache.H, cache.d):
+        raise PowerAttnError(f"q must be bfloat16 {[cache.B, cache.H, cache.d]} on the pool's device")
+    with _OnDevice(pool.device):
+        p, t = _cache_ptrs(lib, cache, pool, table, "power_attn_cache_step")
+        o = torch.empty_like(q) if out is None else out
+        L = torch.empty(cache.B, cache.H, dtype=torch.float32, device=pool.device) if out_lse is None else out_lse
+        need = int(lib.power_attn_cache_step_workspace_bytes(cache))
+        workspace, ws = _workspace(need, workspace, pool.device)
+        st = lib.power_attn_cache_step(cache, _dev_ptr(q, name="q"), _array_ptr(slopes, q, (cache.H,), torch.float32, "slopes"), p, t,
+                                       _lengths_ptr(lens, pool, cache, "lens"), _shaped_ptr(o, q, q.shape, "o"),
+                                       _array_ptr(L, pool, (cache.B, cache.H), torch.float32, "L"), ws, need, _stream())
+    if st != 0:
+        _check(lib, st, "power_attn_cache_step")
+    return o, L

@@ -1,0 +1,920 @@
+// The paged cache of keys and values that exponential attention decodes from: rows in (rotated on the way), values out, one token's
+// attention for every sequence.
+//
+// A page holds, per key head, keys and values in the order in which the matrix instructions of a step (v_mfma_f32_16x16x32) want
+// them as their A operand, so a step's loads go from memory to the operand's registers, 16 bytes a lane and 1 KB of consecutive
+// memory a wave, with nothing transposed on the way.  With lane l = 16 g + r of that operand (row r, k-slots 8 g .. 8 g + 7):
+//   keys, S^T = K Q^T: rows are 16 tokens, k-slots 32 channels.   16 bits: [token / 16][channel / 32][l] of 16 bytes
+//   values, O^T = V^T P^T: rows are 16 channels, k-slots the 32 tokens of a unit, in the order in which the accumulators of the
+//     first product hold them: slot e of lane group g is token 4 g + e % 4 + 16 (e / 4).   16 bits: [unit][channel / 16][l] of 16 bytes
+//   4 bits, keys: [token / 16][l][channel / 32] words of 8 codes, code e in nibble e / 2 + 4 (e % 2), so that a shift and a mask give two
+//     k-slots; then [token][unit of each 32 channels, minimum of each] fp16
+//   4 bits, values: [unit][channel / 64][l] of 8 slots of 16 bits, in nibble n of a slot channel 64 () + 16 n + r; then
+//     [unit][channel / 32][g][unit of 8 slots, minimum of 8 slots] fp16
+#include <algorithm>
+#include <type_traits>
+
+#include "mfma_common.hpp"
+
+namespace pa {
+namespace mfma {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+constexpr int UNIT = 32;                // tokens of the values' layout, and of a step's inner loop
+constexpr int QGROUP = 32;              // channels of one scale and minimum
+constexpr float Q_LIMIT = 65024.f;      // values of a 4-bit cache: minimum + 15 units, both rounded, stays in fp16's range
+
+template <int HD, int BITS>
+struct Layout {
+    // bytes per token and key head
+    static constexpr int CODES = HD * BITS / 8, PARAMS = BITS == 4 ? HD / 8 : 0, TOKEN = 2 * (CODES + PARAMS);
+    // keys, their parameters, values, their parameters, from the start of a page's block of one head
+    __device__ static __forceinline__ size_t k_params(int page) { return (size_t)page * CODES; }
+    __device__ static __forceinline__ size_t values(int page) { return (size_t)page * (CODES + PARAMS); }
+    __device__ static __forceinline__ size_t v_params(int page) { return (size_t)page * (2 * CODES + PARAMS); }
+    __device__ static __forceinline__ size_t block(int page) { return (size_t)page * TOKEN; }
+};
+
+struct Pages {
+    const int* table;
+    int page, shift;            // tokens per page, log2
+    int max_pages, num_pages, Hk;
+};
+// page of token position pos (0 <= pos < max_pages page) of sequence b, -1 where the table has none
+__device__ __forceinline__ int page_of(const Pages& pg, int b, int pos) {
+    const int id = pg.table[(size_t)b * pg.max_pages + (pos >> pg.shift)];
+    return (unsigned)id < (unsigned)pg.num_pages ? id : -1;
+}
+
+// ---- 8 channels of a row -----------------------------------------------------------------------------------
+__device__ __forceinline__ void unpack8(float (&x)[8], uint4 u) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = bf_lo(w[i]);
+        x[2 * i + 1] = bf_hi(w[i]);
+    }
+}
+__device__ __forceinline__ uint4 pack8(const float (&x)[8]) {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f.v[i] = (__bf16)x[i];
+    return f.u;
+}
+struct Rotation {
+    const float *cos, *sin;     // [rows][rot / 2]
+    int rot, adjacent;
+};
+// Channels 8 c8 .. + 7 of a row at table row pos, rotated; every operation rounded on its own, so that the values (and the
+// codes made of them) are those of the formula.
+template <int HD>
+__device__ __forceinline__ void rotated8(float (&x)[8], const bf16_t* row, int c8, int pos, const Rotation& ro) {
+#pragma clang fp contract(off)
+    unpack8(x, *(const uint4*)(row + 8 * c8));
+    if (8 * c8 >= ro.rot) return;
+    const int half = ro.rot / 2;
+    const size_t at = (size_t)pos * half;
+    if (ro.adjacent) {
+        const float4 c = *(const float4*)(ro.cos + at + 4 * c8), s = *(const float4*)(ro.sin + at + 4 * c8);
+        const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float a = x[2 * i], b = x[2 * i + 1];
+            x[2 * i] = a * cc[i] - b * ss[i];
+            x[2 * i + 1] = b * cc[i] + a * ss[i];
+        }
+        return;
+    }
+    const bool second = 8 * c8 >= half;
+    const int first = 8 * c8 - (second ? half : 0);         // the angle's number
+    float y[8];
+    unpack8(y, *(const uint4*)(row + (second ? first : first + half)));
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+        const float4 c = *(const float4*)(ro.cos + at + first + 4 * q), s = *(const float4*)(ro.sin + at + first + 4 * q);
+        const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float mine = x[4 * q + i] * cc[i], other = y[4 * q + i] * ss[i];
+            x[4 * q + i] = second ? mine + other : mine - other;
+        }
+    }
+}
+template <int CTRL>
+__device__ __forceinline__ float quad(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, false));
+}
+// The group's unit and minimum and this lane's 8 codes, the group being this lane's 8 channels and those of the other lanes of its quad
+struct Held {
+    float unit, least;      // as fp16 holds them
+    uint32_t code[8];
+};
+__device__ __forceinline__ void hold8(Held& to, const float (&x)[8]) {
+#pragma clang fp contract(off)
+    float lo = x[0], hi = x[0];
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        lo = fminf(lo, x[i]);
+        hi = fmaxf(hi, x[i]);
+        nan |= x[i] != x[i];
+    }
+    lo = nan ? __builtin_nanf("") : fminf(fmaxf(lo, -Q_LIMIT), Q_LIMIT);
+    hi = fminf(fmaxf(hi, -Q_LIMIT), Q_LIMIT);
+    // NaN wins
+    auto least = [](float a, float b) { return a != a || b != b ? __builtin_nanf("") : fminf(a, b); };
+    lo = least(lo, quad<0xB1>(lo));
+    hi = fmaxf(hi, quad<0xB1>(hi));
+    lo = least(lo, quad<0x4E>(lo));
+    hi = fmaxf(hi, quad<0x4E>(hi));
+    to.unit = (float)(_Float16)((hi - lo) / 15.f);
+    to.least = (float)(_Float16)lo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float v = fminf(fmaxf(x[i], -Q_LIMIT), Q_LIMIT);
+        const float c = to.unit > 0.f ? __builtin_rintf((v - to.least) / to.unit) : 0.f;
+        to.code[i] = (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
+    }
+}
+__device__ __forceinline__ bf16_t half_bits(float x) {
+    union {
+        _Float16 h;
+        bf16_t u;
+    } c;
+    c.h = (_Float16)x;
+    return c.u;
+}
+__device__ __forceinline__ float half_value(uint32_t u) {
+    union {
+        bf16_t u;
+        _Float16 h;
+    } c;
+    c.u = (bf16_t)u;
+    return (float)c.h;
+}
+// 16 bytes of 8 slots (tokens 4 g + e % 4 + 16 (e / 4) of a unit): whole where all of them are written
+__device__ __forceinline__ void store_slots(char* dst, const bf16_t (&x)[8], uint32_t take) {
+    if (take == 0xffu) {
+        union {
+            bf16_t h[8];
+            uint4 u;
+        } o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o.h[e] = x[e];
+        *(uint4*)dst = o.u;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (take >> e & 1) ((bf16_t*)dst)[e] = x[e];
+    }
+}
+__device__ __forceinline__ int slot_token(int g, int e) { return 4 * g + (e & 3) + 16 * (e >> 2); }
+// the slots of lane group g among the tokens of a unit
+__device__ __forceinline__ uint32_t slots_of(uint32_t tokens, int g) { return (tokens >> (4 * g) & 0xfu) | (tokens >> (4 * g + 16) & 0xfu) << 4; }
+
+// ---- rows in -------------------------------------------------------------------------------------------------
+// A workgroup takes the tokens of one unit (32 positions of a page) of one head: y < Hk a key head, the others a query head that is
+// only rotated.  Keys go straight to their place, values through LDS, where a unit's 8 slots come together.
+struct Take {
+    int b, first;           // sequence; position of the unit's first token
+    int t0;                 // row of the call at that position (may be negative)
+    uint32_t tokens;        // the unit's tokens that the call has rows for
+};
+__device__ __forceinline__ bool take_unit(Take& t, const Pages& pg, const int* from, const int* count, int T) {
+    t.b = (int)blockIdx.z;
+    const int start = from[t.b], cap = pg.max_pages << pg.shift;
+    const int n = count != nullptr ? min(count[t.b], T) : T;
+    if (start >= cap || start <= -(1 << 30)) return false;      // (rows number less than 2^30)
+    t.first = ((start >> 5) + (int)blockIdx.x) * UNIT;
+    if (t.first < 0 || t.first >= cap) return false;
+    t.t0 = t.first - start;
+    const int lo = max(0, -t.t0), hi = min(UNIT, n - t.t0);     // of the unit
+    if (lo >= hi) return false;
+    t.tokens = (hi == 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
+    return true;
+}
+
+template <int HD, int BITS>
+__global__ __launch_bounds__(256) void k_cache_append(const bf16_t* __restrict__ K, const bf16_t* __restrict__ V, const bf16_t* Q, bf16_t* Q_out,
+                                                      char* __restrict__ pool, const int* __restrict__ past,
+                                                      const int* __restrict__ count, int T, int H, Pages pg, Rotation ro, int key_heads) {
+    using Lay = Layout<HD, BITS>;
+    constexpr int PIECES = HD / 8, PER = 256 / PIECES;      // lanes per row, rows per pass
+    __shared__ __attribute__((aligned(16))) bf16_t rows[UNIT][HD + 8];
+    __shared__ bf16_t params[2][UNIT][HD / QGROUP];
+    Take t;
+    if (!take_unit(t, pg, past, count, T)) return;
+    const int tid = threadIdx.x, c8 = tid % PIECES, y = (int)blockIdx.y;
+    if (y >= key_heads) {
+        const size_t row0 = ((size_t)t.b * H + (y - key_heads)) * T;
+#pragma unroll
+        for (int p = 0; p < UNIT; p += PER) {
+            const int tok = p + tid / PIECES;
+            if (!(t.tokens >> tok & 1)) continue;
+            float x[8];
+            const size_t row = row0 + t.t0 + tok;
+            rotated8<HD>(x, Q + row * HD, c8, t.first + tok, ro);
+            // (Q_out may be Q: a row's lanes are of one wave, which has loaded before it stores)
+            *(uint4*)(Q_out + row * HD + 8 * c8) = pack8(x);
+        }
+        return;
+    }
+    const int id = page_of(pg, t.b, t.first);
+    if (id < 0) return;
+    char* block = pool + ((size_t)id * pg.Hk + y) * Lay::block(pg.page);
+    const int in_page = t.first & (pg.page - 1);
+    const size_t row0 = ((size_t)t.b * pg.Hk + y) * T;
+#pragma unroll
+    for (int p = 0; p < UNIT; p += PER) {
+        const int tok = p + tid / PIECES;
+        if (!(t.tokens >> tok & 1)) continue;
+        const size_t row = row0 + t.t0 + tok;
+        float x[8];
+        rotated8<HD>(x, K + row * HD, c8, t.first + tok, ro);
+        const uint4 v = *(const uint4*)(V + row * HD + 8 * c8);
+        const int blk = (in_page + tok) / 16, r = tok % 16, ks = c8 / 4, g = c8 % 4;
+        if (BITS == 16) {
+            *(uint4*)(block + (((size_t)blk * (HD / 32) + ks) * 64 + 16 * g + r) * 16) = pack8(x);
+            *(uint4*)&rows[tok][8 * c8] = v;
+        } else {
+            Held h;
+            hold8(h, x);
+            uint32_t word = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) word |= h.code[e] << (4 * (e / 2 + 4 * (e % 2)));
+            *(uint32_t*)(block + (((size_t)blk * 64 + 16 * g + r) * (HD / 32) + ks) * 4) = word;
+            bf16_t* kp = (bf16_t*)(block + Lay::k_params(pg.page)) + (size_t)(in_page + tok) * (HD / 16);
+            if (g == 0) kp[ks] = half_bits(h.unit);
+            if (g == 1) kp[HD / 32 + ks] = half_bits(h.least);
+            unpack8(x, v);
+            hold8(h, x);
+            union {
+                bf16_t c[8];
+                uint4 u;
+            } codes;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) codes.c[e] = (bf16_t)h.code[e];
+            *(uint4*)&rows[tok][8 * c8] = codes.u;
+            if (g == 0) params[0][tok][ks] = half_bits(h.unit);
+            if (g == 1) params[1][tok][ks] = half_bits(h.least);
+        }
+    }
+    __syncthreads();
+    const int unit = in_page / UNIT;
+    char* values = block + Lay::values(pg.page);
+    if (BITS == 16) {
+        for (int n = tid; n < HD / 16 * 64; n += 256) {
+            const int l = n % 64, cb = n / 64, g = l / 16;
+            const uint32_t take = slots_of(t.tokens, g);
+            bf16_t x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = rows[slot_token(g, e)][16 * cb + l % 16];
+            store_slots(values + (((size_t)unit * (HD / 16) + cb) * 64 + l) * 16, x, take);
+        }
+    } else {
+        for (int n = tid; n < HD / 64 * 64; n += 256) {
+            const int l = n % 64, hf = n / 64, g = l / 16;
+            const uint32_t take = slots_of(t.tokens, g);
+            bf16_t x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t w = 0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w |= (uint32_t)rows[slot_token(g, e)][64 * hf + 16 * c + l % 16] << (4 * c);
+                x[e] = (bf16_t)w;
+            }
+            store_slots(values + (((size_t)unit * (HD / 64) + hf) * 64 + l) * 16, x, take);
+        }
+        // parameters: the other threads
+        const int n = 255 - tid;
+        if (n < HD / 32 * 8) {
+            const int which = n % 2, g = n / 2 % 4, cg = n / 8;
+            bf16_t x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = params[which][slot_token(g, e)][cg];
+            store_slots(block + Lay::v_params(pg.page) + ((((size_t)unit * (HD / 32) + cg) * 4 + g) * 2 + which) * 16, x, slots_of(t.tokens, g));
+        }
+    }
+}
+
+// ---- values out ------------------------------------------------------------------------------------------------
+template <int HD, int BITS>
+__global__ __launch_bounds__(256) void k_cache_read(const char* __restrict__ pool, const int* __restrict__ start,
+                                                    const int* __restrict__ count, bf16_t* __restrict__ K, bf16_t* __restrict__ V,
+                                                    int T, Pages pg) {
+    using Lay = Layout<HD, BITS>;
+    constexpr int PIECES = HD / 8, PER = 256 / PIECES;
+    __shared__ __attribute__((aligned(16))) bf16_t rows[UNIT][HD + 8];
+    Take t;
+    if (!take_unit(t, pg, start, count, T)) return;
+    const int tid = threadIdx.x, c8 = tid % PIECES, hk = (int)blockIdx.y;
+    const int id = page_of(pg, t.b, t.first);
+    const char* block = pool + ((size_t)max(id, 0) * pg.Hk + hk) * Lay::block(pg.page);
+    const int in_page = t.first & (pg.page - 1), unit = in_page / UNIT;
+    const size_t row0 = ((size_t)t.b * pg.Hk + hk) * T;
+    const char* values = block + Lay::values(pg.page);
+    if (id >= 0) {
+        if (BITS == 16) {
+            for (int n = tid; n < HD / 16 * 64; n += 256) {
+                const int l = n % 64, cb = n / 64;
+                union {
+                    uint4 u;
+                    bf16_t h[8];
+                } x;
+                x.u = *(const uint4*)(values + (((size_t)unit * (HD / 16) + cb) * 64 + l) * 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) rows[slot_token(l / 16, e)][16 * cb + l % 16] = x.h[e];
+            }
+        } else {
+            // (lane, nibble) of a 16-byte piece
+            for (int n = tid; n < HD / 64 * 256; n += 256) {
+                const int l = n % 64, c = n / 64 % 4, hf = n / 256, g = l / 16, cg = 2 * hf + c / 2;
+                union {
+                    uint4 u;
+                    bf16_t h[8];
+                } x, un, le;
+                x.u = *(const uint4*)(values + (((size_t)unit * (HD / 64) + hf) * 64 + l) * 16);
+                const char* par = block + Lay::v_params(pg.page) + (((size_t)unit * (HD / 32) + cg) * 4 + g) * 32;
+                un.u = *(const uint4*)par;
+                le.u = *(const uint4*)(par + 16);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    rows[slot_token(g, e)][64 * hf + 16 * c + l % 16] =
+                        f32_to_bf16(fmaf((float)(x.h[e] >> (4 * c) & 15), half_value(un.h[e]), half_value(le.h[e])));
+            }
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < UNIT; p += PER) {
+        const int tok = p + tid / PIECES;
+        if (!(t.tokens >> tok & 1)) continue;
+        const size_t at = (row0 + t.t0 + tok) * HD + 8 * c8;
+        uint4 k = make_uint4(0, 0, 0, 0), v = k;
+        if (id >= 0) {
+            const int blk = (in_page + tok) / 16, r = tok % 16, ks = c8 / 4, g = c8 % 4;
+            v = *(const uint4*)&rows[tok][8 * c8];
+            if (BITS == 16) {
+                k = *(const uint4*)(block + (((size_t)blk * (HD / 32) + ks) * 64 + 16 * g + r) * 16);
+            } else {
+                const uint32_t word = *(const uint32_t*)(block + (((size_t)blk * 64 + 16 * g + r) * (HD / 32) + ks) * 4);
+                const bf16_t* kp = (const bf16_t*)(block + Lay::k_params(pg.page)) + (size_t)(in_page + tok) * (HD / 16);
+                const float u = half_value(kp[ks]), m = half_value(kp[HD / 32 + ks]);
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = fmaf((float)(word >> (4 * (e / 2 + 4 * (e % 2))) & 15), u, m);
+                k = pack8(x);
+            }
+        }
+        *(uint4*)(K + at) = k;
+        *(uint4*)(V + at) = v;
+    }
+}
+
+// ---- one token's attention -----------------------------------------------------------------------------------------
+// Work is cut on the device, since lengths are known there only: the visible units of all sequences together are dealt in chunks of
+// one size, so that long sequences get more workgroups than short ones and a captured launch follows the lengths of its replay.
+// A sequence of one chunk is finished by its workgroup; the parts of the others are joined by a second kernel.
+constexpr int CHUNK_MIN = 4;            // units: one for each wave
+struct Split {
+    int target;             // chunks that the units are dealt to (a sequence's last chunk may be shorter: up to B more)
+    int slots;              // target + B
+};
+struct Visible {
+    int len, first;         // tokens held, first token seen
+    int unit0, units;
+};
+__device__ __forceinline__ Visible visible(const int* lens, int b, int B, const Pages& pg, int window) {
+    Visible v{0, 0, 0, 0};
+    if (b < B) {
+        v.len = min(max(lens[b], 0), pg.max_pages << pg.shift);
+        v.first = window > 0 ? max(0, v.len - window) : 0;
+        v.unit0 = v.first / UNIT;
+        v.units = (v.len + UNIT - 1) / UNIT - v.unit0;
+    }
+    return v;
+}
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) x += __shfl_xor(x, off);
+    return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_scan(int x, int lane) {     // inclusive
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(x, off);
+        if (lane >= off) x += y;
+    }
+    return x;
+}
+__device__ __forceinline__ int chunk_units(const int* lens, int B, const Pages& pg, int window, int target, int lane) {
+    // (64-bit: lengths up to 2^30 of many sequences)
+    unsigned long long total = 0;
+    for (int base = 0; base < B; base += 64) {
+        const int u = visible(lens, base + lane, B, pg, window).units;
+        total += (unsigned)wave_sum(u & 0xffff) + ((unsigned long long)(unsigned)wave_sum(u >> 16) << 16);
+    }
+    const unsigned long long c = (total + target - 1) / target;
+    return max(CHUNK_MIN, (int)min(c, 1ULL << 26));     // (a sequence has at most 2^25 units)
+}
+
+template <int BITS>
+struct Elem {
+    typedef bf16x8 vec;
+};
+template <>
+struct Elem<4> {
+    typedef f16x8 vec;
+};
+__device__ __forceinline__ f32x4 mfma_step(bf16x8 a, bf16x8 b, f32x4 c) { return mfma16(a, b, c); }
+__device__ __forceinline__ f32x4 mfma_step(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// two codes (nibbles `at` / 4 of both halves) as fp16: 1024 + c has c in its last bits
+template <int AT>
+__device__ __forceinline__ f16x2 codes2(uint32_t w) {
+    union {
+        uint32_t u;
+        f16x2 h;
+    } x;
+    if (AT == 0 || AT == 8) {
+        x.u = ((AT == 8 ? w >> 8 : w) & 0x000f000fu) | 0x64006400u;
+        return x.h - (f16x2){1024, 1024};
+    }
+    x.u = ((AT == 12 ? w >> 8 : w) & 0x00f000f0u) | 0x64006400u;       // 1024 + 16 c
+    return __builtin_elementwise_fma(x.h, (f16x2){0.0625f, 0.0625f}, (f16x2){-64, -64});
+}
+
+// A unit's operands as they lie in memory, and as the products take them
+template <int HD, int BITS>
+struct Keys;
+template <int HD, int BITS>
+struct Values;
+template <int HD>
+struct Keys<HD, 16> {
+    Frag f[2][HD / 32];
+    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
+        const char* p = block + ((size_t)unit * 2 * (HD / 32) * 64 + lane) * 16;
+#pragma unroll
+        for (int n = 0; n < 2 * (HD / 32); ++n) f[n / (HD / 32)][n % (HD / 32)].u = *(const uint4*)(p + n * 1024);
+    }
+    __device__ __forceinline__ bf16x8 operand(int blk, int ks) const { return f[blk][ks].v; }
+};
+template <int HD>
+struct Values<HD, 16> {
+    Frag f[HD / 16];
+    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
+        const char* p = block + Layout<HD, 16>::values(pg.page) + ((size_t)unit * (HD / 16) * 64 + lane) * 16;
+#pragma unroll
+        for (int n = 0; n < HD / 16; ++n) f[n].u = *(const uint4*)(p + n * 1024);
+    }
+    // slots whose token is not seen hold zeros: their weight is 0, but what memory holds there may be no number
+    __device__ __forceinline__ void keep(uint32_t slots) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!(slots >> e & 1))
+#pragma unroll
+                for (int n = 0; n < HD / 16; ++n) f[n].v[e] = (__bf16)0.f;
+    }
+    __device__ __forceinline__ bf16x8 operand(int cb) const { return f[cb].v; }
+};
+template <int HD>
+struct Keys<HD, 4> {
+    uint32_t w[2][HD / 32];
+    _Float16 u[2][HD / 32], m[2][HD / 32];
+    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
+        const char* p = block + ((size_t)unit * 2 * 64 + lane) * (HD / 8);
+        const char* q = block + Layout<HD, 4>::k_params(pg.page) + (size_t)(unit * UNIT + lane % 16) * (HD / 8);
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            if constexpr (HD == 128) {
+                const uint4 x = *(const uint4*)(p + blk * 64 * 16);
+                w[blk][0] = x.x; w[blk][1] = x.y; w[blk][2] = x.z; w[blk][3] = x.w;
+                const f16x8 h = *(const f16x8*)(q + blk * 16 * 16);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    u[blk][k] = h[k];
+                    m[blk][k] = h[4 + k];
+                }
+            } else {
+                typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+                const uint2 x = *(const uint2*)(p + blk * 64 * 8);
+                w[blk][0] = x.x; w[blk][1] = x.y;
+                const f16x4 h = *(const f16x4*)(q + blk * 16 * 8);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    u[blk][k] = h[k];
+                    m[blk][k] = h[2 + k];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ f16x8 operand(int blk, int ks) const {
+        const f16x2 u2 = {u[blk][ks], u[blk][ks]}, m2 = {m[blk][ks], m[blk][ks]};
+        const uint32_t x = w[blk][ks];
+        union {
+            f16x2 h[4];
+            f16x8 v;
+        } o;
+        o.h[0] = __builtin_elementwise_fma(codes2<0>(x), u2, m2);
+        o.h[1] = __builtin_elementwise_fma(codes2<4>(x), u2, m2);
+        o.h[2] = __builtin_elementwise_fma(codes2<8>(x), u2, m2);
+        o.h[3] = __builtin_elementwise_fma(codes2<12>(x), u2, m2);
+        return o.v;
+    }
+};
+template <int HD>
+struct Values<HD, 4> {
+    uint4 c[HD / 64];
+    f16x8 u[HD / 32], m[HD / 32];
+    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
+        const char* p = block + Layout<HD, 4>::values(pg.page) + ((size_t)unit * (HD / 64) * 64 + lane) * 16;
+        const char* q = block + Layout<HD, 4>::v_params(pg.page) + ((size_t)unit * (HD / 32) * 4 + lane / 16) * 32;
+#pragma unroll
+        for (int n = 0; n < HD / 64; ++n) c[n] = *(const uint4*)(p + n * 1024);
+#pragma unroll
+        for (int n = 0; n < HD / 32; ++n) {
+            u[n] = *(const f16x8*)(q + n * 128);
+            m[n] = *(const f16x8*)(q + n * 128 + 16);
+        }
+    }
+    __device__ __forceinline__ void keep(uint32_t slots) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!(slots >> e & 1))
+#pragma unroll
+                for (int n = 0; n < HD / 32; ++n) u[n][e] = m[n][e] = 0;
+    }
+    __device__ __forceinline__ f16x8 operand(int cb) const {
+        const uint4 x = c[cb / 4];
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        const f16x8 un = u[cb / 2], le = m[cb / 2];
+        union {
+            f16x2 h[4];
+            f16x8 v;
+        } o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f16x2 k;
+            switch (cb % 4) {
+                case 0: k = codes2<0>(w[i]); break;
+                case 1: k = codes2<4>(w[i]); break;
+                case 2: k = codes2<8>(w[i]); break;
+                default: k = codes2<12>(w[i]); break;
+            }
+            o.h[i] = __builtin_elementwise_fma(k, (f16x2){un[2 * i], un[2 * i + 1]}, (f16x2){le[2 * i], le[2 * i + 1]});
+        }
+        return o.v;
+    }
+};
+
+struct StepScore {
+    float sl, kc, capl;     // as in exp_attn.hip: scale log2 e; 2 scale log2 e / cap; cap log2 e
+};
+// Weights are exp2(s - ref), ref 7 below a maximum met so far and moved once a score is 15 above it: as fp16 weights up to 2^15 and down to
+// 2^-24, which is 2^-31 of the largest, are there.
+constexpr float REF_BELOW = 7.f, REF_MOVE = 15.f;
+constexpr float STEP_NONE = -__builtin_inff();
+
+template <int HD, int BITS, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q, const float* __restrict__ slopes,
+                                                    const char* __restrict__ pool, const int* __restrict__ lens, bf16_t* __restrict__ o,
+                                                    float* __restrict__ L, float* __restrict__ part, float2* __restrict__ stat, int B,
+                                                    int H, int G, int window, Pages pg, Split split, StepScore sc) {
+    using Lay = Layout<HD, BITS>;
+    using vec = typename Elem<BITS>::vec;
+    constexpr int NK = HD / 32, NV = HD / 16;
+    __shared__ __attribute__((aligned(16))) float sum[4][16][HD + 4];
+    __shared__ float2 ml[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
+    // blocks of 16 query heads of a key head side by side: they read the same pages
+    const int mblks = (G + 15) / 16, per = pg.Hk * mblks;
+    const int slot = (int)(blockIdx.x / (unsigned)per), rest = (int)(blockIdx.x - (unsigned)slot * (unsigned)per);
+    const int hk = rest / mblks, mb = rest - hk * mblks;
+
+    // the slot's sequence and place in it
+    const int C = chunk_units(lens, B, pg, window, split.target, lane);
+    int b = -1, nth = 0, chunks = 0, before = 0;
+    Visible vis{0, 0, 0, 0};
+    for (int base = 0; base < B && b < 0; base += 64) {
+        const Visible v = visible(lens, base + lane, B, pg, window);
+        const int n = (v.units + C - 1) / C, upto = before + wave_scan(n, lane);
+        const uint64_t past = __ballot(upto > slot);
+        if (past != 0) {
+            const int at = __builtin_ctzll(past);
+            b = base + at;
+            chunks = __builtin_amdgcn_readlane(n, at);
+            nth = slot - (__builtin_amdgcn_readlane(upto, at) - chunks);
+            vis = {__builtin_amdgcn_readlane(v.len, at), __builtin_amdgcn_readlane(v.first, at), __builtin_amdgcn_readlane(v.unit0, at),
+                   __builtin_amdgcn_readlane(v.units, at)};
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    if (b < 0) return;
+    const int u_end = vis.unit0 + min(vis.units, (nth + 1) * C);       // (nth + 1) C <= units + C, and both are below 2^26
+    int u = vis.unit0 + nth * C + w;
+
+    // the head of this lane's column
+    const int hq = 16 * mb + r16, head = hk * G + min(hq, G - 1);
+    vec qf[NK];
+    float factor = 1.f;
+    {
+        Frag raw[NK];
+        float top = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < NK; ++ks) {
+            raw[ks].u = *(const uint4*)(q + ((size_t)b * H + head) * HD + 32 * ks + 8 * g);
+            if (hq >= G) raw[ks].u = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)raw[ks].v[e]));
+        }
+        if constexpr (BITS == 16) {
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) qf[ks] = raw[ks].v;
+        } else {
+            // q over a power of two, so that bf16's range fits fp16's; the scores take it back
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const int ex = top > 0.f && top < __builtin_inff() ? ilogbf(top) : 0;
+            factor = ldexpf(1.f, ex);
+            const float inv = ldexpf(1.f, -ex);
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) qf[ks][e] = (_Float16)((float)raw[ks].v[e] * inv);
+        }
+    }
+    const float slope = BIAS ? slopes[head] * 1.44269504088896340736f : 0.f;
+    const float mul = (CAP ? sc.kc : sc.sl) * factor;
+
+    f32x4 acc[NV];
+#pragma unroll
+    for (int cb = 0; cb < NV; ++cb) acc[cb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float ref = STEP_NONE, lsum = 0.f;
+
+    auto unit = [&](auto edge_c, const Keys<HD, BITS>& kk, Values<HD, BITS>& vv, int at, auto&& then) {
+        constexpr bool EDGE = decltype(edge_c)::value;
+        f32x4 s[2];
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            s[blk] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(kk.operand(blk, ks), qf[ks], s[blk]);
+        }
+        then();         // the keys' registers are free
+        const int tok0 = at * UNIT + 4 * g;
+        const float far = BIAS ? (float)(vis.len - 1 - tok0) : 0.f;
+        float x[8], top = STEP_NONE;
+        uint32_t slots = 0xffu;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int tok = (e & 3) + 16 * (e >> 2);
+            float y = s[e >> 2][e & 3] * mul;
+            if (CAP) y = fmaf(-2.f * sc.capl, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f), sc.capl);
+            if (BIAS) y = fmaf(-slope, far - (float)tok, y);
+            if (EDGE && (tok0 + tok >= vis.len || tok0 + tok < vis.first)) {
+                y = STEP_NONE;
+                slots &= ~(1u << e);
+            }
+            x[e] = y;
+            top = fmaxf(top, y);
+        }
+        if (__any(top > ref + REF_MOVE)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float to = fmaxf(ref, top - REF_BELOW);
+            const float f = to == STEP_NONE ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+            ref = to;
+            lsum *= f;
+#pragma unroll
+            for (int cb = 0; cb < NV; ++cb)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[cb][r] *= f;
+        }
+        const float by = ref == STEP_NONE ? 0.f : ref;
+        vec p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (BITS == 16) p[e] = (__bf16)__builtin_amdgcn_exp2f(x[e] - by);
+            else p[e] = (_Float16)__builtin_amdgcn_exp2f(x[e] - by);
+            lsum += (float)p[e];        // the weights that the products use
+        }
+        if (EDGE) vv.keep(slots);
+#pragma unroll
+        for (int cb = 0; cb < NV; ++cb) acc[cb] = mfma_step(vv.operand(cb), p, acc[cb]);
+    };
+
+    // Page numbers of the wave's next 64 units, one a lane.  Keys and values of the next unit are asked for as soon as their registers are
+    // free, one product ahead.
+    Keys<HD, BITS> kk;
+    Values<HD, BITS> vv;
+    const int upp = pg.page / UNIT;
+    while (u < u_end) {
+        const int mine = u + 4 * lane;
+        const int ids = mine < u_end ? page_of(pg, b, mine * UNIT) : -1;
+        const int n = min(64, (u_end - u + 3) / 4);
+        uint64_t have = __ballot(ids >= 0);
+        if (n < 64) have &= (1ULL << n) - 1;
+        auto block_of = [&](int i) {
+            const int id = __builtin_amdgcn_readlane(ids, i);
+            return pool + ((size_t)id * pg.Hk + hk) * Lay::block(pg.page);
+        };
+        if (have != 0) {
+            int i = __builtin_ctzll(have);
+            kk.load(block_of(i), pg, (u + 4 * i) & (upp - 1), lane);
+            vv.load(block_of(i), pg, (u + 4 * i) & (upp - 1), lane);
+            while (have != 0) {
+                have &= have - 1;
+                const int at = u + 4 * i, next = have != 0 ? __builtin_ctzll(have) : i;
+                const char* block = block_of(next);
+                const int in = (u + 4 * next) & (upp - 1);
+                auto then = [&]() {
+                    if (have != 0) kk.load(block, pg, in, lane);
+                };
+                if (at * UNIT < vis.first || at * UNIT + UNIT > vis.len) unit(std::true_type{}, kk, vv, at, then);
+                else unit(std::false_type{}, kk, vv, at, then);
+                if (have != 0) vv.load(block, pg, in, lane);
+                i = next;
+            }
+        }
+        u += 256;
+    }
+
+    // the four waves' parts
+    lsum += __shfl_xor(lsum, 16);
+    lsum += __shfl_xor(lsum, 32);
+    if (g == 0) ml[w][r16] = make_float2(ref, lsum);
+#pragma unroll
+    for (int cb = 0; cb < NV; ++cb) *(f32x4*)&sum[w][r16][16 * cb + 4 * g] = acc[cb];
+    __syncthreads();
+    constexpr int LPH = 16;             // lanes per head
+    const int h = tid / LPH, c0 = tid % LPH;
+    if (16 * mb + h >= G) return;
+    float top = STEP_NONE, z = 0.f, f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i][h].x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = ml[i][h].x == STEP_NONE ? (ml[i][h].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[i][h].x - top);
+        z += f[i] * ml[i][h].y;
+    }
+    const int hd = hk * G + 16 * mb + h;
+    const float inv = chunks == 1 ? (z != 0.f ? 1.f / z : 0.f) : 1.f;
+#pragma unroll
+    for (int c = 4 * c0; c < HD; c += 4 * LPH) {
+        f32x4 x = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 y = *(const f32x4*)&sum[i][h][c];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] += f[i] * y[r];
+        }
+        if (chunks == 1) {
+            bf16x4 y;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[r] = (__bf16)(x[r] * inv);
+            *(bf16x4*)(o + ((size_t)b * H + hd) * HD + c) = y;
+        } else {
+            *(f32x4*)(part + ((size_t)slot * H + hd) * HD + c) = x;
+        }
+    }
+    if (c0 == 0) {
+        if (chunks > 1) stat[(size_t)slot * H + hd] = make_float2(top, z);
+        else if (L != nullptr) L[(size_t)b * H + hd] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.69314718055994530942f : STEP_NONE;
+    }
+}
+
+// sequences of several chunks; those of none get what an empty row has.  A wave per query head.
+template <int HD>
+__global__ __launch_bounds__(256) void k_cache_join(const int* __restrict__ lens, const float* __restrict__ part,
+                                                    const float2* __restrict__ stat, bf16_t* __restrict__ o, float* __restrict__ L, int B,
+                                                    int H, int window, Pages pg, Split split) {
+    constexpr int PER = HD / 64;
+    const int lane = threadIdx.x & 63;
+    const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (long long)B * H) return;
+    const int b = __builtin_amdgcn_readfirstlane((int)(row / H)), h = __builtin_amdgcn_readfirstlane((int)(row % H));
+    const int C = chunk_units(lens, B, pg, window, split.target, lane);
+    int first = 0, chunks = 0;
+    for (int base = 0; base <= b; base += 64) {
+        const int n = (visible(lens, base + lane, B, pg, window).units + C - 1) / C;
+        first += wave_sum(base + lane < b ? n : 0);
+        if (b - base < 64) chunks = __builtin_amdgcn_readlane(n, b - base);
+    }
+    if (chunks == 1) return;
+    float top = STEP_NONE;
+    for (int i = lane; i < chunks; i += 64) top = fmaxf(top, stat[(size_t)(first + i) * H + h].x);
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+    float z = 0.f, x[PER];
+#pragma unroll
+    for (int c = 0; c < PER; ++c) x[c] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < chunks; ++i) {
+        const size_t at = (size_t)(first + i) * H + h;
+        const float2 s = stat[at];
+        const float f = s.x == STEP_NONE ? (s.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(s.x - top);
+        z += f * s.y;
+#pragma unroll
+        for (int c = 0; c < PER; ++c) x[c] += f * part[at * HD + PER * lane + c];
+    }
+    const float inv = z != 0.f ? 1.f / z : 0.f;
+#pragma unroll
+    for (int c = 0; c < PER; ++c) o[(size_t)row * HD + PER * lane + c] = f32_to_bf16(x[c] * inv);
+    if (lane == 0 && L != nullptr) L[row] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.69314718055994530942f : STEP_NONE;
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+Pages pages_of(const pa_cache& c, const int* table) {
+    int shift = 0;
+    while ((1 << shift) < c.page) ++shift;
+    return {table, c.page, shift, c.max_pages, c.num_pages, c.Hk};
+}
+Split split_of(const pa_cache& c) {
+    const int per = c.Hk * ((c.H / c.Hk + 15) / 16);
+    const int target = std::max(1, 1024 / per);
+    return {target, target + c.B};
+}
+size_t part_bytes(const pa_cache& c) { return align_up((size_t)split_of(c).slots * c.H * c.d * sizeof(float), 256); }
+
+template <typename F>
+pa_status dispatch(const pa_cache& c, F f) {
+    auto with = [&](auto hd) {
+        return c.bits == 4 ? f(hd, std::integral_constant<int, 4>{}) : f(hd, std::integral_constant<int, 16>{});
+    };
+    return c.d == 128 ? with(std::integral_constant<int, 128>{}) : with(std::integral_constant<int, 64>{});
+}
+unsigned units_over(int T) { return (unsigned)((T + 30) / 32 + 1); }     // units that T rows from any position can touch
+
+}  // namespace
+}  // namespace mfma
+
+using namespace mfma;
+
+size_t cache_bytes(const pa_cache& c) {
+    const size_t token = c.bits == 16 ? 4 * (size_t)c.d : 2 * ((size_t)c.d / 2 + c.d / 8);
+    return (size_t)c.num_pages * c.Hk * c.page * token;
+}
+size_t cache_step_workspace_bytes(const pa_cache& c) {
+    return part_bytes(c) + align_up((size_t)split_of(c).slots * c.H * sizeof(float2), 256);
+}
+
+pa_status cache_append(const pa_cache& c, int T, const bf16_t* K, const bf16_t* V, const bf16_t* Q, bf16_t* Q_out, const float* cos,
+                       const float* sin, void* pool, const int* table, const int* past, const int* count, hipStream_t s) {
+    const int key_heads = K != nullptr ? c.Hk : 0, heads = key_heads + (Q != nullptr ? c.H : 0);
+    LaunchScope ls("cache_append", s);
+    return dispatch(c, [&](auto hd, auto bits) {
+        hipLaunchKernelGGL((k_cache_append<decltype(hd)::value, decltype(bits)::value>), dim3(units_over(T), (unsigned)heads, (unsigned)c.B),
+                           dim3(256), 0, s, K, V, Q, Q_out, (char*)pool, past, count, T, c.H, pages_of(c, table),
+                           Rotation{cos, sin, c.rot, c.rot_adjacent}, key_heads);
+        return launch_ok() ? PA_OK : PA_ERR_HIP;
+    });
+}
+
+pa_status cache_read(const pa_cache& c, int T, const void* pool, const int* table, const int* start, const int* count, bf16_t* K,
+                     bf16_t* V, hipStream_t s) {
+    LaunchScope ls("cache_read", s);
+    return dispatch(c, [&](auto hd, auto bits) {
+        hipLaunchKernelGGL((k_cache_read<decltype(hd)::value, decltype(bits)::value>), dim3(units_over(T), (unsigned)c.Hk, (unsigned)c.B),
+                           dim3(256), 0, s, (const char*)pool, start, count, K, V, T, pages_of(c, table));
+        return launch_ok() ? PA_OK : PA_ERR_HIP;
+    });
+}
+
+pa_status cache_step(const pa_cache& c, const bf16_t* q, const float* slopes, const void* pool, const int* table, const int* lens,
+                     bf16_t* o, float* L, char* ws, hipStream_t s) {
+    const Split split = split_of(c);
+    const int G = c.H / c.Hk, window = c.window;
+    const Pages pg = pages_of(c, table);
+    float* part = (float*)ws;
+    float2* stat = (float2*)(ws + part_bytes(c));
+    StepScore sc{c.scale * 1.44269504088896340736f, 0.f, 0.f};
+    if (c.cap > 0.f) {
+        sc.kc = (float)(2.0 * c.scale / c.cap * 1.44269504088896340736);
+        sc.capl = c.cap * 1.44269504088896340736f;
+    }
+    const unsigned grid = (unsigned)split.slots * (unsigned)(c.Hk * ((G + 15) / 16));
+    auto launch = [&](auto hd, auto bits, auto cap, auto bias) {
+        LaunchScope ls("cache_step", s);
+        hipLaunchKernelGGL((k_cache_step<decltype(hd)::value, decltype(bits)::value, decltype(cap)::value, decltype(bias)::value>), dim3(grid),
+                           dim3(256), 0, s, q, slopes, (const char*)pool, lens, o, L, part, stat, c.B, c.H, G, window, pg, split, sc);
+        return launch_ok() ? PA_OK : PA_ERR_HIP;
+    };
+    const pa_status st = dispatch(c, [&](auto hd, auto bits) {
+        if (c.cap > 0.f)
+            return slopes != nullptr ? launch(hd, bits, std::true_type{}, std::true_type{}) : launch(hd, bits, std::true_type{}, std::false_type{});
+        return slopes != nullptr ? launch(hd, bits, std::false_type{}, std::true_type{}) : launch(hd, bits, std::false_type{}, std::false_type{});
+    });
+    if (st != PA_OK) return st;
+    LaunchScope ls("cache_join", s);
+    const unsigned rows = (unsigned)(((long long)c.B * c.H + 3) / 4);
+    if (c.d == 128)
+        hipLaunchKernelGGL((k_cache_join<128>), dim3(rows), dim3(256), 0, s, lens, part, stat, o, L, c.B, c.H, window, pg, split);
+    else
+        hipLaunchKernelGGL((k_cache_join<64>), dim3(rows), dim3(256), 0, s, lens, part, stat, o, L, c.B, c.H, window, pg, split);
+    return launch_ok() ? PA_OK : PA_ERR_HIP;
+}
+
+}  // namespace pa

@@ -151,4 +151,26 @@ size_t mfma_gate_slots(const pa_problem& pr);
 // gate_gradient
 int mfma_gate_fin_chunk(const pa_problem& pr, const char* ws, int& xparts, const float*& dotk);
 
+// exponential attention (exp_attn.hip); slopes, lo and hi may be null
+struct ExpMask {
+    const float* slopes;
+    const int *lo, *hi;
+};
+bool exp_grid_ok(const pa_exp_problem& pr);     // the launches fit a grid
+size_t exp_workspace_bytes(const pa_exp_problem& pr, bool backward);
+pa_status exp_fwd(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, const bf16_t* V, ExpMask mask, bf16_t* O, float* L,
+                  char* ws, hipStream_t s);
+pa_status exp_bwd(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, const bf16_t* V, ExpMask mask, const bf16_t* O,
+                  const float* L, const bf16_t* dO, bf16_t* dQ, bf16_t* dK, bf16_t* dV, char* ws, hipStream_t s);
+
+// the paged cache that it decodes from (cache.hip)
+size_t cache_bytes(const pa_cache& c);
+pa_status cache_append(const pa_cache& c, int T, const bf16_t* K, const bf16_t* V, const bf16_t* Q, bf16_t* Q_out, const float* cos,
+                       const float* sin, void* pool, const int* table, const int* past, const int* count, hipStream_t s);
+pa_status cache_read(const pa_cache& c, int T, const void* pool, const int* table, const int* start, const int* count, bf16_t* K,
+                     bf16_t* V, hipStream_t s);
+size_t cache_step_workspace_bytes(const pa_cache& c);
+pa_status cache_step(const pa_cache& c, const bf16_t* q, const float* slopes, const void* pool, const int* table, const int* lens,
+                     bf16_t* o, float* L, char* ws, hipStream_t s);
+
 }  // namespace pa

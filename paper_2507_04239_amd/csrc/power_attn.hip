@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
 #include <string>
 #include <vector>
 
@@ -454,6 +455,135 @@ pa_status power_attn_decode_step(const pa_problem* prob, const void* q, const vo
     if (state == nullptr || state_bytes < need) return PA_ERR_WORKSPACE;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(state)) return PA_ERR_INVALID_ARG;
     return decode_step(*prob, q, k, v, log_g, state, o, z, (hipStream_t)hip_stream);
+}
+
+// ---- exponential attention and its cache ----
+static bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+
+// score and window of pa_exp_problem and pa_cache; with a cap 2 scale / cap is a factor of its own, in units of log 2
+static bool score_ok(float scale, float cap, int window) {
+    if (!std::isfinite(scale) || !(scale > 0.f) || !std::isfinite(cap) || !(cap >= 0.f) || window < 0) return false;
+    const float most = 1e38f;
+    return scale <= most && cap <= most && (cap == 0.f || 2.0 * scale / cap <= most);
+}
+static pa_status validate_exp(const pa_exp_problem* pr) {
+    if (pr == nullptr) return PA_ERR_INVALID_ARG;
+    if (pr->B <= 0 || pr->H <= 0 || pr->Hk <= 0 || pr->T <= 0 || pr->Tk <= 0 || pr->d <= 0 || pr->H % pr->Hk != 0) return PA_ERR_INVALID_ARG;
+    if (!score_ok(pr->scale, pr->cap, pr->window)) return PA_ERR_INVALID_ARG;
+    if (pr->dtype != PA_DTYPE_F32 && pr->dtype != PA_DTYPE_BF16) return PA_ERR_INVALID_ARG;
+    if (pr->dtype != PA_DTYPE_BF16 || (pr->d != 32 && pr->d != 64 && pr->d != 128)) return PA_ERR_UNSUPPORTED;
+    if (pr->T > (1 << 30) || pr->Tk > (1 << 30) || (long long)pr->B * pr->H > 0x7fffffffLL || !exp_grid_ok(*pr)) return PA_ERR_UNSUPPORTED;
+    return PA_OK;
+}
+
+pa_status power_attn_exp_supported(const pa_exp_problem* prob, int) { return validate_exp(prob); }
+
+size_t power_attn_exp_workspace_bytes(const pa_exp_problem* prob, int for_backward) {
+    return validate_exp(prob) == PA_OK ? exp_workspace_bytes(*prob, for_backward != 0) : 0;
+}
+
+static pa_status exp_workspace_ok(const pa_exp_problem& pr, bool backward, const void* workspace, size_t bytes) {
+    const size_t need = exp_workspace_bytes(pr, backward);
+    if (need > 0 && (workspace == nullptr || bytes < need)) return PA_ERR_WORKSPACE;
+    return ((uintptr_t)workspace & 255u) != 0 ? PA_ERR_WORKSPACE : PA_OK;
+}
+
+pa_status power_attn_exp_fwd(const pa_exp_problem* prob, const void* Q, const void* K, const void* V, const float* slopes,
+                             const int* row_lo, const int* row_hi, void* O, float* L, void* workspace, size_t workspace_bytes,
+                             void* hip_stream) {
+    pa_status st = validate_exp(prob);
+    if (st != PA_OK) return st;
+    if (Q == nullptr || K == nullptr || V == nullptr || O == nullptr) return PA_ERR_INVALID_ARG;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned4(L) || !aligned4(slopes) || !aligned4(row_lo) ||
+        !aligned4(row_hi))
+        return PA_ERR_INVALID_ARG;
+    st = exp_workspace_ok(*prob, false, workspace, workspace_bytes);
+    if (st != PA_OK) return st;
+    (void)hipGetLastError();
+    return exp_fwd(*prob, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, ExpMask{slopes, row_lo, row_hi}, (bf16_t*)O, L,
+                   (char*)workspace, (hipStream_t)hip_stream);
+}
+
+pa_status power_attn_exp_bwd(const pa_exp_problem* prob, const void* Q, const void* K, const void* V, const float* slopes,
+                             const int* row_lo, const int* row_hi, const void* O, const float* L, const void* dO, void* dQ, void* dK,
+                             void* dV, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    pa_status st = validate_exp(prob);
+    if (st != PA_OK) return st;
+    if (Q == nullptr || K == nullptr || V == nullptr || O == nullptr || L == nullptr || dO == nullptr || dQ == nullptr || dK == nullptr ||
+        dV == nullptr)
+        return PA_ERR_INVALID_ARG;
+    if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(dO) || !aligned16(dQ) || !aligned16(dK) ||
+        !aligned16(dV) || !aligned4(L) || !aligned4(slopes) || !aligned4(row_lo) || !aligned4(row_hi))
+        return PA_ERR_INVALID_ARG;
+    st = exp_workspace_ok(*prob, true, workspace, workspace_bytes);
+    if (st != PA_OK) return st;
+    (void)hipGetLastError();
+    return exp_bwd(*prob, (const bf16_t*)Q, (const bf16_t*)K, (const bf16_t*)V, ExpMask{slopes, row_lo, row_hi}, (const bf16_t*)O, L,
+                   (const bf16_t*)dO, (bf16_t*)dQ, (bf16_t*)dK, (bf16_t*)dV, (char*)workspace, (hipStream_t)hip_stream);
+}
+
+static pa_status validate_cache(const pa_cache* c) {
+    if (c == nullptr) return PA_ERR_INVALID_ARG;
+    if (c->B <= 0 || c->H <= 0 || c->Hk <= 0 || c->d <= 0 || c->H % c->Hk != 0 || c->max_pages <= 0 || c->num_pages <= 0)
+        return PA_ERR_INVALID_ARG;
+    if (c->page < 32 || c->page > 1024 || (c->page & (c->page - 1)) != 0 || (c->bits != 16 && c->bits != 4)) return PA_ERR_INVALID_ARG;
+    if (c->rot < 0 || c->rot > c->d || c->rot % 16 != 0 || (c->rot_adjacent != 0 && c->rot_adjacent != 1)) return PA_ERR_INVALID_ARG;
+    if (!score_ok(c->scale, c->cap, c->window)) return PA_ERR_INVALID_ARG;
+    const long long positions = (long long)c->max_pages * c->page;
+    if (c->rot > 0 && c->rot_rows < positions) return PA_ERR_INVALID_ARG;
+    if ((c->d != 64 && c->d != 128) || positions > (1 << 30) || c->B > 65535 || c->H + c->Hk > 65535 ||
+        (long long)c->B * c->H > (1 << 30))
+        return PA_ERR_UNSUPPORTED;
+    return PA_OK;
+}
+
+size_t power_attn_cache_bytes(const pa_cache* cache) { return validate_cache(cache) == PA_OK ? cache_bytes(*cache) : 0; }
+
+pa_status power_attn_cache_append(const pa_cache* cache, int T, const void* K, const void* V, const void* Q, void* Q_out,
+                                  const float* cos, const float* sin, void* pool, const int* table, const int* past,
+                                  const int* count, void* hip_stream) {
+    pa_status st = validate_cache(cache);
+    if (st != PA_OK) return st;
+    if (T <= 0 || past == nullptr || table == nullptr || (K == nullptr) != (V == nullptr) || (K == nullptr && Q == nullptr))
+        return PA_ERR_INVALID_ARG;
+    if ((K != nullptr && pool == nullptr) || (Q != nullptr && Q_out == nullptr)) return PA_ERR_INVALID_ARG;
+    if (cache->rot > 0 && (cos == nullptr || sin == nullptr)) return PA_ERR_INVALID_ARG;
+    if (!aligned16(K) || !aligned16(V) || !aligned16(Q) || !aligned16(Q_out) || !aligned16(cos) || !aligned16(sin) || !aligned16(pool) ||
+        !aligned4(table) || !aligned4(past) || !aligned4(count))
+        return PA_ERR_INVALID_ARG;
+    if (T > (1 << 29)) return PA_ERR_UNSUPPORTED;
+    (void)hipGetLastError();
+    return cache_append(*cache, T, (const bf16_t*)K, (const bf16_t*)V, (const bf16_t*)Q, (bf16_t*)Q_out, cos, sin, pool, table, past,
+                        count, (hipStream_t)hip_stream);
+}
+
+pa_status power_attn_cache_read(const pa_cache* cache, int T, const void* pool, const int* table, const int* start, const int* count,
+                                void* K, void* V, void* hip_stream) {
+    pa_status st = validate_cache(cache);
+    if (st != PA_OK) return st;
+    if (T <= 0 || pool == nullptr || table == nullptr || start == nullptr || K == nullptr || V == nullptr) return PA_ERR_INVALID_ARG;
+    if (!aligned16(pool) || !aligned16(K) || !aligned16(V) || !aligned4(table) || !aligned4(start) || !aligned4(count))
+        return PA_ERR_INVALID_ARG;
+    if (T > (1 << 29)) return PA_ERR_UNSUPPORTED;
+    (void)hipGetLastError();
+    return cache_read(*cache, T, pool, table, start, count, (bf16_t*)K, (bf16_t*)V, (hipStream_t)hip_stream);
+}
+
+size_t power_attn_cache_step_workspace_bytes(const pa_cache* cache) {
+    return validate_cache(cache) == PA_OK ? cache_step_workspace_bytes(*cache) : 0;
+}
+
+pa_status power_attn_cache_step(const pa_cache* cache, const void* q, const float* slopes, const void* pool, const int* table,
+                                const int* lens, void* o, float* L, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    pa_status st = validate_cache(cache);
+    if (st != PA_OK) return st;
+    if (q == nullptr || pool == nullptr || table == nullptr || lens == nullptr || o == nullptr) return PA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(pool) || !aligned16(o) || !aligned4(slopes) || !aligned4(table) || !aligned4(lens) || !aligned4(L))
+        return PA_ERR_INVALID_ARG;
+    if (workspace == nullptr || workspace_bytes < cache_step_workspace_bytes(*cache) || ((uintptr_t)workspace & 255u) != 0)
+        return PA_ERR_WORKSPACE;
+    (void)hipGetLastError();
+    return cache_step(*cache, (const bf16_t*)q, slopes, pool, table, lens, (bf16_t*)o, L, (char*)workspace, (hipStream_t)hip_stream);
 }
 
 int power_attn_resolved_chunk(const pa_problem* prob) {

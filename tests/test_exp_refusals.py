@@ -1,0 +1,114 @@
+"""What exponential attention and the paged cache refuse, seen without a GPU: nothing is launched."""
+import ctypes
+import math
+import os
+
+import pytest
+
+from paper_2507_04239_amd import binding as pa
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(pa.library_path()):
+        import __graft_entry__ as g
+        g.build()
+    return pa.load_library()
+
+
+OK = dict(B=1, H=4, Hk=2, T=10, Tk=20, d=64, scale=1.0, cap=0.0, window=0, dtype="bf16")
+
+
+@pytest.mark.parametrize("status,change", [
+    (1, dict(B=0)), (1, dict(H=0)), (1, dict(Hk=0)), (1, dict(T=0)), (1, dict(Tk=-1)), (1, dict(d=0)), (1, dict(H=5)), (1, dict(Hk=8)),
+    (1, dict(scale=0.0)), (1, dict(scale=-1.0)), (1, dict(scale=math.nan)), (1, dict(scale=math.inf)), (1, dict(cap=-1.0)),
+    (1, dict(cap=math.nan)), (1, dict(cap=math.inf)), (1, dict(cap=1e-40)), (1, dict(window=-1)), (2, dict(d=48)), (2, dict(d=256)),
+    (2, dict(dtype="f32")), (2, dict(T=2 ** 30 + 1)), (2, dict(Tk=2 ** 31 - 1)), (2, dict(B=2 ** 20, H=2 ** 12, Hk=2 ** 12)),
+    (2, dict(B=2 ** 15, T=2 ** 28)),
+])
+def test_problems(lib, status, change):
+    prob = pa.make_exp_problem(**{**OK, **change})
+    p = ctypes.c_void_p(4096)
+    assert lib.power_attn_exp_supported(prob, 0) == status and lib.power_attn_exp_workspace_bytes(prob, 1) == 0
+    assert lib.power_attn_exp_fwd(prob, p, p, p, None, None, None, p, p, p, 1 << 40, None) == status
+    assert lib.power_attn_exp_bwd(prob, p, p, p, None, None, None, p, p, p, p, p, p, p, 1 << 40, None) == status
+
+
+def test_pointers_and_workspaces(lib):
+    prob = pa.make_exp_problem(**OK)
+    assert lib.power_attn_exp_supported(prob, 1) == 0
+    need = lib.power_attn_exp_workspace_bytes(prob, 1)
+    assert need > 0
+    a = ctypes.c_void_p(4096)
+    fwd = [a, a, a, None, None, None, a, None, a, 1 << 40, None]
+    for i in (0, 1, 2, 6):
+        for bad in (None, ctypes.c_void_p(4096 + 8)):
+            assert lib.power_attn_exp_fwd(prob, *[bad if n == i else x for n, x in enumerate(fwd)]) == 1
+    for i in (3, 4, 5, 7):
+        assert lib.power_attn_exp_fwd(prob, *[ctypes.c_void_p(4098) if n == i else x for n, x in enumerate(fwd)]) == 1
+    bwd = [a, a, a, None, None, None, a, a, a, a, a, a, a, need, None]
+    for i in (0, 1, 2, 6, 7, 8, 9, 10, 11):
+        assert lib.power_attn_exp_bwd(prob, *[None if n == i else x for n, x in enumerate(bwd)]) == 1
+    assert lib.power_attn_exp_bwd(prob, *bwd[:12], None, need, None) == 3
+    assert lib.power_attn_exp_bwd(prob, *bwd[:12], a, need - 1, None) == 3
+    assert lib.power_attn_exp_bwd(prob, *bwd[:12], ctypes.c_void_p(4096 + 16), need, None) == 3
+    assert lib.power_attn_exp_fwd(None, *fwd) == 1 and lib.power_attn_exp_supported(None, 0) == 1
+
+
+CACHE = dict(B=2, H=4, Hk=2, d=64, page=64, max_pages=4, num_pages=9, bits=4, rot=32, rot_rows=256, scale=1.0)
+
+
+@pytest.mark.parametrize("status,change", [
+    (1, dict(B=0)), (1, dict(H=3)), (1, dict(Hk=0)), (1, dict(d=-1)), (1, dict(page=0)), (1, dict(page=16)), (1, dict(page=96)),
+    (1, dict(page=2048)), (1, dict(max_pages=0)), (1, dict(num_pages=0)), (1, dict(bits=8)), (1, dict(rot=8)), (1, dict(rot=-16)),
+    (1, dict(rot=80)), (1, dict(rot_rows=255)), (1, dict(scale=0.0)), (1, dict(cap=-1.0)), (1, dict(window=-1)), (2, dict(d=32)),
+    (2, dict(d=256)), (2, dict(max_pages=2 ** 25, rot=0)), (2, dict(B=65536)), (2, dict(H=65535, Hk=1)),
+])
+def test_caches(lib, status, change):
+    c = pa.make_cache(**{**CACHE, **change})
+    p = ctypes.c_void_p(4096)
+    assert lib.power_attn_cache_bytes(c) == 0 and lib.power_attn_cache_step_workspace_bytes(c) == 0
+    assert lib.power_attn_cache_append(c, 1, p, p, p, p, p, p, p, p, p, None, None) == status
+    assert lib.power_attn_cache_read(c, 1, p, p, p, None, p, p, None) == status
+    assert lib.power_attn_cache_step(c, p, None, p, p, p, p, None, p, 1 << 40, None) == status
+
+
+def test_cache_sizes(lib):
+    c = pa.make_cache(**CACHE)
+    assert pa.power_attn_cache_bytes(c) == 9 * 2 * 64 * 2 * (32 + 8)      # codes and parameters of keys and values
+    assert pa.power_attn_cache_bytes(pa.make_cache(**{**CACHE, "bits": 16})) == 9 * 2 * 64 * 2 * 128
+    assert pa.power_attn_cache_bytes(pa.make_cache(**{**CACHE, "num_pages": 2 ** 22})) == 2 ** 22 * 2 * 64 * 80
+
+
+def test_cache_arguments(lib):
+    c = pa.make_cache(**CACHE)
+    a, odd = ctypes.c_void_p(4096), ctypes.c_void_p(4096 + 8)
+    append = [1, a, a, a, a, a, a, a, a, a, None, None]
+    for i in (1, 2, 4, 5, 6, 7, 8, 9):      # K or V alone, Q without a place, no angles, pool, table, past
+        assert lib.power_attn_cache_append(c, *[None if n == i else x for n, x in enumerate(append)]) == 1, i
+    for i in (1, 2, 3, 4, 5, 6, 7):
+        assert lib.power_attn_cache_append(c, *[odd if n == i else x for n, x in enumerate(append)]) == 1, i
+    assert lib.power_attn_cache_append(c, 0, *append[1:]) == 1
+    assert lib.power_attn_cache_append(c, 2 ** 29 + 1, *append[1:]) == 2
+    assert lib.power_attn_cache_append(c, 1, None, None, None, None, *append[5:]) == 1
+    read = [1, a, a, a, None, a, a, None]
+    for i in (1, 2, 3, 5, 6):
+        assert lib.power_attn_cache_read(c, *[None if n == i else x for n, x in enumerate(read)]) == 1, i
+    need = lib.power_attn_cache_step_workspace_bytes(c)
+    step = [a, None, a, a, a, a, None, a, need, None]
+    for i in (0, 2, 3, 4, 5):
+        assert lib.power_attn_cache_step(c, *[None if n == i else x for n, x in enumerate(step)]) == 1, i
+    assert lib.power_attn_cache_step(c, *step[:7], None, need, None) == 3
+    assert lib.power_attn_cache_step(c, *step[:7], a, need - 1, None) == 3
+    assert lib.power_attn_cache_step(c, *step[:7], odd, need, None) == 3
+
+
+def test_binding_checks_shapes():
+    import torch
+    q, k = torch.zeros(1, 4, 5, 64), torch.zeros(1, 2, 5, 64)
+    with pytest.raises(pa.PowerAttnError, match="GPU"):
+        pa.power_attn_exp_fwd(q, k, k)
+    with pytest.raises(pa.PowerAttnError):
+        pa._exp_plan_of(0, q, k, torch.zeros(1, 2, 6, 64), 1.0, 0.0, 0)
+    with pytest.raises(pa.PowerAttnError):
+        pa._exp_plan_of(0, q, torch.zeros(1, 2, 5, 32), torch.zeros(1, 2, 5, 32), 1.0, 0.0, 0)

@@ -1,0 +1,371 @@
+"""The paged cache: what goes in comes out, and a step's attention against float64 within the bounds that the oracle derives."""
+import math
+
+import pytest
+import torch
+
+from oracle.exp_attn_oracle import exp_attn, held4, rotated
+from paper_2507_04239_amd import binding as pa
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def tables(n, rot, base=10000.0):
+    angle = torch.arange(n, dtype=torch.float64)[:, None] * base ** (-torch.arange(rot // 2, dtype=torch.float64) / max(rot // 2, 1))
+    return angle.cos().float(), angle.sin().float()
+
+
+class Cache:
+    """A cache with its pool full of NaN, a shuffled table, and the plain copy of what it holds."""
+
+    def __init__(self, B, H, Hk, d, page, pages, bits, seed=0, rot=0, adjacent=False, spare=3, **score):
+        gen = torch.Generator().manual_seed(seed)
+        self.B, self.H, self.Hk, self.d, self.bits, self.page = B, H, Hk, d, bits, page
+        num = B * pages + spare
+        self.c = pa.make_cache(B, H, Hk, d, page, pages, num, bits=bits, rot=rot, rot_adjacent=adjacent,
+                               rot_rows=pages * page if rot else 0, **score)
+        self.score = score
+        self.pool = torch.full((pa.power_attn_cache_bytes(self.c),), 0xff, dtype=torch.uint8, device=DEV)      # NaN in fp16 and bf16
+        self.table = torch.randperm(num, generator=gen)[:B * pages].int().view(B, pages).to(DEV)
+        self.rot, self.adjacent = rot, adjacent
+        self.cos, self.sin = tables(pages * page, rot) if rot else (None, None)
+        self.k = torch.full((B, Hk, pages * page, d), math.nan)
+        self.v = torch.full((B, Hk, pages * page, d), math.nan)
+
+    def ints(self, x):
+        return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+    def append(self, K, V, past, count=None, Q=None, **more):
+        """bf16 CPU tensors; also into the plain copy"""
+        B, T = self.B, (K if K is not None else Q).shape[2]
+        on = lambda x: None if x is None else x.to(DEV)
+        got = pa.power_attn_cache_append(self.c, on(K), on(V), self.pool, self.table, self.ints(past), None if count is None else self.ints(count),
+                                         Q=on(Q), cos=on(self.cos), sin=on(self.sin), **more)
+        if K is not None:
+            for b in range(B):
+                for t in range(T if count is None else min(count[b], T)):
+                    p = past[b] + t
+                    if 0 <= p < self.k.shape[2]:
+                        k = K[b, :, t].float()
+                        if self.rot:
+                            k = rotated(k[:, None], torch.tensor([p]), self.cos, self.sin, self.adjacent)[:, 0]
+                        self.k[b, :, p] = self.hold(k)
+                        self.v[b, :, p] = self.hold(V[b, :, t].float())
+        return got
+
+    def hold(self, x):
+        return x.bfloat16().float() if self.bits == 16 else held4(x)
+
+    def read(self, start, T, count=None):
+        out = [torch.full((self.B, self.Hk, T, self.d), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        pa.power_attn_cache_read(self.c, self.pool, self.table, self.ints(start), T, None if count is None else self.ints(count), out=out)
+        return [x.float().cpu() for x in out]
+
+    def fill(self, lens, seed=0):
+        gen = torch.Generator().manual_seed(seed)
+        T = max(1, max(lens))
+        K, V = (torch.randn(self.B, self.Hk, T, self.d, generator=gen).bfloat16() for _ in range(2))
+        self.append(K, V, [0] * self.B, [max(n, 0) for n in lens])
+
+    def step(self, q, lens, slopes=None, **more):
+        out = torch.full((self.B, self.H, self.d), math.nan, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((self.B, self.H), math.nan, device=DEV)
+        o, L = pa.power_attn_cache_step(self.c, q.to(DEV), self.pool, self.table, self.ints(lens),
+                                        slopes=None if slopes is None else slopes.to(DEV), out=out, out_lse=lse, **more)
+        return o.float().cpu(), L.cpu()
+
+    def check_step(self, q, lens, slopes=None, see=None):
+        """see: per sequence the positions that are there (all of lens without)"""
+        o, L = self.step(q, lens, slopes)
+        for b in range(self.B):
+            n = min(max(lens[b], 0), self.k.shape[2])
+            if n == 0:
+                assert not o[b].any() and (L[b] == -math.inf).all(), b
+                continue
+            lo, k, v = None, self.k[b:b + 1, :, :n], self.v[b:b + 1, :, :n]
+            want = exp_attn(q[b:b + 1, :, None], k, v, slopes=slopes, held=0.0 if self.bits == 16 else 2.0 ** -11, **self.score)
+            for got, name in ((o[b], "O"), (L[b], "L")):
+                w, e = want[name][0].squeeze(1), want["e" + name][0].squeeze(1)
+                off = (got.double() - w).abs()
+                assert (off <= e).all(), (b, n, name, float((off / e).max()))
+
+
+def queries(B, H, d, seed=1, sharp=2.0):
+    return (torch.randn(B, H, d, generator=torch.Generator().manual_seed(seed)) * sharp).bfloat16()
+
+
+def same(x, y):
+    return ((x == y) | (x.isnan() & y.isnan())).all()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rot,adjacent", [(0, False), (16, False), (64, False), (64, True), (32, True)])
+def test_what_goes_in_comes_out(bits, d, rot, adjacent):
+    """Ragged calls from odd positions; rows that no call has are left alone in Q_out and in what is read."""
+    c = Cache(3, 5, 1, d, 32, 4, bits, rot=rot, adjacent=adjacent)
+    gen = torch.Generator().manual_seed(d + rot)
+    for T, past, count in ((50, [0, 3, 31], [50, 20, 0]), (1, [50, 23, 31], None), (40, [51, 100, 90], [7, 40, 99]), (3, [126, -2, 200], None)):
+        K, V, Q = (torch.randn(3, h, T, d, generator=gen).bfloat16() for h in (1, 1, 5))
+        out = torch.full((3, 5, T, d), 7.0, dtype=torch.bfloat16, device=DEV)
+        got = c.append(K, V, past, count, Q=Q, out_q=out).float().cpu()
+        for b in range(3):
+            for t in range(T):
+                if t < (T if count is None else count[b]) and 0 <= past[b] + t < 128:
+                    x = Q[b, :, t].float()
+                    x = rotated(x[:, None], torch.tensor([past[b] + t]), c.cos, c.sin, adjacent)[:, 0] if rot else x
+                    assert torch.equal(got[b, :, t], x.bfloat16().float()), (b, t)
+                else:
+                    assert (got[b, :, t] == 7.0).all(), (b, t)
+    k, v = c.read([0, 0, 0], 128)
+    assert not c.k[0, :, :58].isnan().any()
+    for b in range(3):
+        there = ~c.k[b, 0, :, 0].isnan()
+        assert torch.equal(k[b][:, there], c.k[b][:, there].bfloat16().float()) and torch.equal(v[b][:, there], c.v[b][:, there].bfloat16().float())
+    k, v = c.read([5, -3, 120], 30, [30, 10, 30])
+    for b, (at, n) in enumerate(((5, 30), (-3, 10), (120, 30))):
+        for t in range(30):
+            p = at + t
+            if t < n and 0 <= p < 128:
+                if not c.k[b, 0, p, 0].isnan():
+                    assert torch.equal(k[b, :, t], c.k[b, :, p].bfloat16().float()), (b, t)
+            else:
+                assert (k[b, :, t] == 7.0).all() and (v[b, :, t] == 7.0).all()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_rows_one_by_one_or_at_once(bits):
+    a, b = (Cache(1, 2, 2, 64, 64, 3, bits, rot=64) for _ in range(2))
+    gen = torch.Generator().manual_seed(5)
+    K, V = (torch.randn(1, 2, 140, 64, generator=gen).bfloat16() for _ in range(2))
+    a.append(K, V, [0])
+    for t in range(140):
+        b.append(K[:, :, t:t + 1], V[:, :, t:t + 1], [t])
+    for x, y in zip(a.read([0], 140), b.read([0], 140)):
+        assert torch.equal(x, y)
+
+
+def test_only_queries_and_in_place():
+    c = Cache(2, 3, 1, 128, 32, 2, 16, rot=128)
+    Q = queries(2 * 3, 40, 128).view(2, 3, 40, 128)
+    want = c.append(None, None, [0, 20], Q=Q)
+    mine = Q.to(DEV)
+    out = pa.power_attn_cache_append(c.c, None, None, c.pool, c.table, c.ints([0, 20]), Q=mine, cos=c.cos.to(DEV), sin=c.sin.to(DEV), out_q=mine)
+    assert out is mine and torch.equal(mine, want)
+    assert (c.pool == 0xff).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_four_bits_at_their_edges(d):
+    """Constant groups, ties, values at and beyond fp16's range, tiny ones, infinities, NaN."""
+    c = Cache(1, 1, 1, d, 32, 2, 4)
+    x = torch.zeros(1, 1, 12, d)
+    x[0, 0, 0] = 3.25
+    x[0, 0, 1] = torch.arange(d) % 32 * 0.5           # halves of a unit
+    x[0, 0, 2], x[0, 0, 2, ::3] = -1e30, 1e30
+    x[0, 0, 3] = torch.linspace(-65024, 65024, d)
+    x[0, 0, 4] = torch.linspace(0, 1e-7, d)
+    x[0, 0, 5, ::5], x[0, 0, 5, 1::5] = math.inf, -math.inf
+    x[0, 0, 6, 40] = math.nan
+    x[0, 0, 7] = torch.linspace(1000, 1001, d)
+    x[0, 0, 8, d - 1] = 1e-30
+    x[0, 0, 9:] = torch.randn(3, d, generator=torch.Generator().manual_seed(1)) * 1e-3
+    x = x.bfloat16()
+    c.append(x, -x, [0])
+    for got, want in zip(c.read([0], 12), (c.k, c.v)):
+        assert same(got[0, 0], want[0, 0, :12].bfloat16().float())
+    assert got[0, 0, 6].isnan().sum() == 32
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [32, 64, 256])
+def test_step_lengths(bits, d, page):
+    lens = [1, 2, 0, 31, 32, 33, -4, 64, 100, 127, 128, 129, 255, 500]
+    c = Cache(len(lens), 4, 2, d, page, (512 + page - 1) // page, bits, scale=d ** -0.5)
+    c.fill(lens)
+    print(bits, d, page, flush=True)
+    c.check_step(queries(len(lens), 4, d), lens)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("cap", [0.0, 3.0])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("window", [0, 1, 40, 333])
+def test_step_scores_and_windows(bits, cap, bias, window):
+    lens = [1, 40, 41, 300, 700]
+    c = Cache(5, 6, 2, 64, 64, 11, bits, scale=0.125, cap=cap, window=window)
+    c.fill(lens)
+    slopes = torch.tensor([0.5, 0.25, 0.1, 0.01, 0.0, -0.001]) if bias else None
+    c.check_step(queries(5, 6, 64, sharp=4.0), lens, slopes)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hk", [(1, 1), (3, 1), (16, 1), (17, 1), (40, 2), (64, 4)])
+def test_step_heads(bits, H, Hk):
+    lens = [130, 77]
+    c = Cache(2, H, Hk, 128, 32, 5, bits, scale=128 ** -0.5)
+    c.fill(lens)
+    c.check_step(queries(2, H, 128), lens)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("B", [1, 3, 70, 200])
+def test_step_long_and_many(bits, B):
+    """One sequence over many workgroups, many sequences over few, lengths far apart."""
+    gen = torch.Generator().manual_seed(B)
+    lens = [int(4000 * torch.rand(1, generator=gen) ** 4) for _ in range(B)]
+    lens[B // 2] = 6000
+    c = Cache(B, 2, 1, 64, 128, 47, bits, scale=0.125)
+    c.fill(lens)
+    c.check_step(queries(B, 2, 64), lens)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_step_of_extreme_values(bits):
+    """Large queries and keys, one key that takes all the weight, then weights far below the largest."""
+    lens = [200, 90]
+    c = Cache(2, 4, 2, 64, 32, 7, bits, scale=1.0)
+    gen = torch.Generator().manual_seed(3)
+    K, V = ((torch.randn(2, 2, 200, 64, generator=gen) * s).bfloat16() for s in (8.0, 1e4))
+    c.append(K, V, [0, 0], lens)
+    c.check_step(queries(2, 4, 64, sharp=8.0), lens)
+    c.check_step(queries(2, 4, 64, sharp=1e-30), lens)
+    c.check_step(torch.zeros(2, 4, 64).bfloat16(), lens)
+    big = Cache(1, 1, 1, 64, 32, 1, bits, scale=1e-6)
+    big.append(K[:1, :1, :20], V[:1, :1, :20], [0])
+    big.check_step(queries(1, 1, 64, sharp=1e5), [20])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_pages_that_are_not_there(bits):
+    """Indices outside the pool: rows are not written, read as zeros, left out of a step."""
+    c = Cache(2, 2, 1, 64, 32, 5, bits, scale=0.125)
+    c.fill([150, 150])
+    for b, col, val in ((0, 1, -1), (0, 3, c.c.num_pages), (1, 0, 2 ** 31 - 1), (1, 4, -2 ** 31)):
+        c.table[b, col] = val
+    k, v = c.read([0, 0], 150)
+    for b, cols in ((0, (1, 3)), (1, (0, 4))):
+        gone = torch.zeros(160, dtype=torch.bool)
+        for col in cols:
+            gone[32 * col:32 * col + 32] = True
+        gone = gone[:150]
+        assert not k[b][:, gone].any() and not v[b][:, gone].any()
+        assert torch.equal(k[b][:, ~gone], c.k[b, :, :150][:, ~gone].bfloat16().float())
+        q = queries(2, 2, 64)
+        o, L = c.step(q, [150, 150])
+        at = torch.nonzero(~gone)[:, 0]
+        want = exp_attn(q[b:b + 1, :, None], c.k[b:b + 1, :, at], c.v[b:b + 1, :, at], scale=0.125, held=2.0 ** -11,
+                        hi=torch.tensor([[len(at)]]))
+        assert ((o[b].double() - want["O"][0, :, 0]).abs() <= want["eO"][0, :, 0]).all()
+        assert ((L[b].double() - want["L"][0, :, 0]).abs() <= want["eL"][0, :, 0]).all()
+    before = c.pool.clone()
+    x = torch.ones(2, 1, 1, 64).bfloat16()
+    c.append(x, x, [33, 130])
+    assert torch.equal(before, c.pool)
+    c.table.fill_(-1)
+    o, L = c.step(q, [150, 3])
+    assert not o.any() and (L == -math.inf).all()
+
+
+def test_lengths_beyond_the_table():
+    c = Cache(1, 2, 1, 64, 32, 2, 16, scale=0.125)
+    c.fill([64])
+    q = queries(1, 2, 64)
+    for x, y in zip(c.step(q, [64]), c.step(q, [2 ** 31 - 1])):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_repeats_streams_and_replays_with_other_lengths(bits):
+    """A captured append and step follow the lengths and tables in place; two graphs share a workspace; another stream.
+    (Positions from 2000 on hold the NaN that the pool came with: a step over them has it too.)"""
+    c = Cache(3, 8, 2, 128, 64, 40, bits, rot=128, scale=128 ** -0.5, cap=10.0)
+    c.fill([2000, 700, 5])
+    gen = torch.Generator().manual_seed(2)
+    K, V, Q = (torch.randn(3, h, 1, 128, generator=gen).bfloat16().to(DEV) for h in (2, 2, 8))
+    past, lens = c.ints([0, 0, 0]), c.ints([0, 0, 0])
+    ws = torch.empty(pa.power_attn_cache_step_workspace_bytes(c.c), dtype=torch.uint8, device=DEV)
+    cos, sin = c.cos.to(DEV), c.sin.to(DEV)
+
+    def token():
+        q = pa.power_attn_cache_append(c.c, K, V, c.pool, c.table, past, Q=Q, cos=cos, sin=sin)
+        return pa.power_attn_cache_step(c.c, q[:, :, 0].contiguous(), c.pool, c.table, lens, workspace=ws)
+
+    def at(n):
+        past.copy_(c.ints(n))
+        lens.copy_(c.ints([x + 1 for x in n]))
+
+    token()
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = token()
+        graphs.append((g, out))
+    side = torch.cuda.Stream()
+    for n in ([1999, 3, 0], [10, 700, 5], [2500, 64, 31], [2559, 0, 0]):
+        at(n)
+        want = [x.clone() for x in token()]
+        again = token()
+        assert all(same(x, y) for x, y in zip(want, again))
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            again = token()
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(same(x, y) for x, y in zip(want, again))
+        for g, out in graphs:
+            for x in out:
+                x.fill_(math.nan)
+            g.replay()
+            assert all(same(x, y) for x, y in zip(want, out)), n
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_prompt_in_pieces_then_tokens(bits):
+    """As they are used together: a prompt in pieces (append, read back, attention of the piece over its context), then token by token; every
+    output is the row that attention over all held rows has."""
+    B, H, Hk, d, T = 1, 4, 2, 64, 230
+    how = dict(scale=0.125, cap=8.0, window=150)
+    c = Cache(B, H, Hk, d, 32, 8, bits, rot=32, **how)
+    gen = torch.Generator().manual_seed(11)
+    K, V = (torch.randn(B, Hk, T, d, generator=gen).bfloat16() for _ in range(2))
+    Q = (torch.randn(B, H, T, d, generator=gen) * 2).bfloat16()
+    slopes = torch.tensor([0.1, 0.02, 0.0, 0.3])
+    outs, qs, at = [], [], 0
+    for n in (70, 1, 99, 30):
+        s = slice(at, at + n)
+        q = c.append(K[:, :, s], V[:, :, s], [at], Q=Q[:, :, s])
+        at += n
+        k, v = pa.power_attn_cache_read(c.c, c.pool, c.table, c.ints([0]), at)
+        outs.append(pa.power_attn_exp_fwd(q, k, v, slopes=slopes.to(DEV), **how)[0].float().cpu())
+        qs.append(q.cpu())
+    for t in range(at, T):
+        q = c.append(K[:, :, t:t + 1], V[:, :, t:t + 1], [t], Q=Q[:, :, t:t + 1])
+        outs.append(c.step(q[:, :, 0].cpu(), [t + 1], slopes)[0][:, :, None])
+        qs.append(q.cpu())
+    got, q = torch.cat(outs, 2).double(), torch.cat(qs, 2)
+    # (a prompt's pieces take 4-bit values as bf16, a token as fp16)
+    want = exp_attn(q, c.k[:, :, :T], c.v[:, :, :T], slopes=slopes, held=0.0 if bits == 16 else 2.0 ** -8, **how)
+    assert ((got - want["O"]).abs() <= want["eO"]).all()
+
+
+@pytest.mark.parametrize("bits,page_bytes", [(16, 4 * 128 * 1024), (4, 160 * 1024)])
+def test_pools_beyond_32_bits(bits, page_bytes):
+    num = (5 << 30) // page_bytes
+    c = pa.make_cache(1, 2, 1, 128, 1024, 2, num, bits=bits, scale=128 ** -0.5)
+    pool = torch.empty(pa.power_attn_cache_bytes(c), dtype=torch.uint8, device=DEV)
+    assert pool.numel() > 2 ** 32
+    small = Cache(1, 2, 1, 128, 1024, 2, bits, scale=128 ** -0.5)
+    small.fill([1100])
+    K, V = (x[:, :, :1100].to(DEV) for x in pa.power_attn_cache_read(small.c, small.pool, small.table, small.ints([0]), 1100))
+    table = torch.tensor([[num - 1, num - 2]], dtype=torch.int32, device=DEV)
+    gen = torch.Generator().manual_seed(0)
+    K, V = (torch.randn(1, 1, 1100, 128, generator=gen).bfloat16().to(DEV) for _ in range(2))
+    pa.power_attn_cache_append(c, K.contiguous(), V.contiguous(), pool, table, small.ints([0]))
+    q = queries(1, 2, 128)
+    o, L = pa.power_attn_cache_step(c, q.to(DEV), pool, table, small.ints([1100]))
+    want = small.step(q, [1100])
+    assert torch.equal(o.float().cpu(), want[0]) and torch.equal(L.cpu(), want[1])

@@ -1,0 +1,228 @@
+"""Exponential attention against float64, element by element within the bounds that the oracle derives."""
+import math
+
+import pytest
+import torch
+
+from oracle.exp_attn_oracle import exp_attn
+from paper_2507_04239_amd.binding import power_attn_exp_bwd, power_attn_exp_fwd
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def make(B, H, Hk, T, Tk, d, seed, sharp=1.5):
+    gen = torch.Generator().manual_seed(seed)
+    q, k, v, g = (torch.randn(B, h, n, d, generator=gen) for h, n in ((H, T), (Hk, Tk), (Hk, Tk), (H, T)))
+    return [x.bfloat16() for x in (q * sharp, k, v, g)]
+
+
+def dev(x):
+    return None if x is None else x.to(DEV)
+
+
+def run(q, k, v, g, **how):
+    how = {n: dev(x) if torch.is_tensor(x) else x for n, x in how.items()}
+    q, k, v, g = (dev(x) for x in (q, k, v, g))
+    out = torch.full_like(q, math.nan), torch.full(q.shape[:3], math.nan, device=DEV)
+    O, L = power_attn_exp_fwd(q, k, v, out=out[0], out_lse=out[1], **how)
+    grads = power_attn_exp_bwd(q, k, v, O, L, g, out=[torch.full_like(x, math.nan) for x in (q, k, v)], **how)
+    return dict(zip(("O", "L", "dQ", "dK", "dV"), (x.float().cpu() for x in (O, L, *grads))))
+
+
+def check(got, want, what=""):
+    for n in ("O", "L", "dQ", "dK", "dV"):
+        x, y, e = got[n].double(), want[n], want["e" + n]
+        same = x == y       # (an empty row's -inf)
+        off = torch.where(same, 0.0, (x - y).abs())
+        assert torch.isfinite(off).all(), (what, n)
+        worst = float((off / e.clamp(min=1e-30)).max())
+        assert worst <= 1.0, (what, n, worst)
+
+
+def both(q, k, v, g, what="", lo=None, hi=None, **how):
+    want = exp_attn(q, k, v, g=g, lo=lo, hi=hi, **how)
+    check(run(q, k, v, g, row_lo=lo, row_hi=hi, **how), want, what)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("T", [1, 2, 31, 64, 65, 128, 129, 300])
+def test_lengths(d, T):
+    print(d, T, flush=True)
+    q, k, v, g = make(1, 2, 2, T, T, d, seed=T + d)
+    both(q, k, v, g, scale=d ** -0.5)
+
+
+@pytest.mark.parametrize("H,Hk", [(4, 1), (6, 2), (8, 8), (3, 3), (9, 3)])
+def test_heads_that_share_a_key_head(H, Hk):
+    q, k, v, g = make(2, H, Hk, 150, 150, 64, seed=H)
+    both(q, k, v, g, scale=0.125, cap=4.0)
+
+
+@pytest.mark.parametrize("T,Tk", [(1, 200), (70, 333), (130, 129), (200, 7), (64, 1)])
+@pytest.mark.parametrize("how", [{}, {"cap": 3.0}, {"window": 20}])
+def test_queries_at_the_end_of_other_keys(T, Tk, how):
+    q, k, v, g = make(1, 2, 1, T, Tk, 64, seed=T)
+    both(q, k, v, g, scale=0.125, **how)
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("cap", [0.0, 2.0, 30.0])
+@pytest.mark.parametrize("bias", [False, True])
+def test_scores(d, cap, bias):
+    q, k, v, g = make(1, 4, 2, 190, 190, d, seed=d, sharp=4.0)
+    both(q, k, v, g, scale=d ** -0.5, cap=cap, slopes=torch.tensor([0.5, 0.06, -0.01, 0.0]) if bias else None)
+
+
+@pytest.mark.parametrize("window", [1, 2, 63, 64, 65, 200, 2 ** 31 - 1])
+def test_windows(window):
+    q, k, v, g = make(1, 2, 1, 260, 260, 64, seed=window % 1000)
+    both(q, k, v, g, scale=0.125, window=window)
+
+
+def documents(B, T, seed, prefix=False, padding=0):
+    gen = torch.Generator().manual_seed(seed)
+    lo, hi = torch.zeros(B, T, dtype=torch.int32), torch.zeros(B, T, dtype=torch.int32)
+    for b in range(B):
+        at = 0
+        while at < T - padding:
+            n = min(int(torch.randint(1, 90, (1,), generator=gen)), T - padding - at)
+            lo[b, at:at + n] = at
+            hi[b, at:at + n] = torch.arange(at + 1, at + n + 1)
+            if prefix:
+                hi[b, at:at + n].clamp_(min=at + (n + 1) // 2)
+            at += n
+    return lo, hi
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("prefix", [False, True])
+@pytest.mark.parametrize("padding", [0, 40, 201])
+def test_documents_prefixes_and_padding(d, prefix, padding):
+    lo, hi = documents(3, 277, d + padding, prefix, padding)
+    q, k, v, g = make(3, 4, 2, 277, 277, d, seed=padding)
+    both(q, k, v, g, scale=d ** -0.5, lo=lo, hi=hi, slopes=torch.tensor([0.1, 0.2, 0.0, 0.3]))
+    both(q, k, v, g, scale=d ** -0.5, lo=lo, hi=hi, window=17, cap=5.0)
+
+
+def test_every_key_seen_and_none():
+    q, k, v, g = make(2, 2, 2, 100, 180, 64, seed=5)
+    full = torch.full((2, 100), 180, dtype=torch.int32)
+    both(q, k, v, g, scale=0.125, hi=full)
+    both(q, k, v, g, scale=0.125, hi=torch.zeros_like(full))
+
+
+def test_ranges_in_any_order():
+    """Intervals that follow no order, and ends that lie outside the keys."""
+    gen = torch.Generator().manual_seed(3)
+    lo, hi = (torch.randint(-50, 350, (2, 200), generator=gen, dtype=torch.int32) for _ in range(2))
+    q, k, v, g = make(2, 2, 1, 200, 300, 64, seed=6)
+    want = exp_attn(q, k, v, g=g, lo=lo, hi=hi, scale=0.125)
+    lo[0, 0], hi[0, 1] = -2 ** 31, 2 ** 31 - 1
+    want = exp_attn(q, k, v, g=g, lo=lo.clamp(0, 300), hi=hi.clamp(0, 300), scale=0.125)
+    check(run(q, k, v, g, row_lo=lo, row_hi=hi, scale=0.125), want)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_what_is_masked_may_hold_anything(bad, d):
+    """Padding, in the middle of tiles, full of NaN or infinities on both sides: the other rows are what they are without."""
+    lo, hi = documents(2, 230, 9, padding=50)
+    q, k, v, g = make(2, 2, 1, 230, 230, d, seed=8)
+    want = exp_attn(q, k, v, g=g, lo=lo, hi=hi, scale=d ** -0.5)
+    for x in (q, k, v, g):
+        x[:, :, 180:] = bad
+    check(run(q, k, v, g, row_lo=lo, row_hi=hi, scale=d ** -0.5), want, bad)
+
+
+@pytest.mark.parametrize("where", ["q", "k", "v", "g"])
+def test_a_nan_reaches_the_rows_that_see_it_and_no_other(where):
+    T, at = 200, 101
+    q, k, v, g = make(1, 1, 1, T, T, 64, seed=12)
+    want = exp_attn(q, k, v, g=g, scale=0.125)
+    {"q": q, "k": k, "v": v, "g": g}[where][0, 0, at, 7] = math.nan
+    got = run(q, k, v, g, scale=0.125)
+    before, after = slice(0, at), slice(at, T)
+    rows = {"q": [at], "k": list(range(at, T)), "v": list(range(at, T)), "g": []}[where]
+    for n in ("O", "dQ"):
+        for i in range(T):
+            x, y, e = got[n][0, 0, i].double(), want[n][0, 0, i], want["e" + n][0, 0, i]
+            if i in rows or (where == "g" and n == "dQ" and i == at):
+                assert torch.isnan(x).any(), (n, i)
+            else:
+                assert ((x - y).abs() <= e).all(), (n, i)
+    # the keys that a spoiled row sees are spoiled, the ones behind it are not
+    spoiled = before if where in "qg" else slice(0, T)
+    for n in ("dK", "dV"):
+        if where in "qg":
+            ok = slice(at + 1, T)
+            assert ((got[n][0, 0, ok].double() - want[n][0, 0, ok]).abs() <= want["e" + n][0, 0, ok]).all(), n
+            assert torch.isnan(got[n][0, 0, spoiled]).any(-1).all(), n
+
+
+def test_extreme_scores():
+    """Rows whose weight sits on one key, caps that are reached, scores that leave the range of exp."""
+    q, k, v, g = make(1, 2, 2, 150, 150, 64, seed=2, sharp=60.0)
+    both(q, k, v, g, scale=1.0)
+    both(q, k, v, g, scale=1.0, cap=1.0)
+    both(q, k, v, g, scale=1.0, cap=500.0)
+
+
+def test_gradients_against_differences():
+    """The oracle's gradients, which the others are held to: loss sum(O dO) at shifted inputs."""
+    q, k, v, g = (x.double() for x in make(1, 2, 1, 20, 23, 32, seed=4))
+    lo, hi = documents(1, 20, 1, prefix=True, padding=3)
+    how = dict(scale=0.2, cap=3.0, slopes=torch.tensor([0.1, 0.3]), lo=lo, hi=hi)
+    want = exp_attn(q, k, v, g=g, **how)
+    loss = lambda *x: float((exp_attn(*x, **how)["O"] * g).sum())
+    gen = torch.Generator().manual_seed(7)
+    for n, name in enumerate(("dQ", "dK", "dV")):
+        x = [q, k, v]
+        dirn = torch.randn(x[n].shape, generator=gen, dtype=torch.float64)
+        up, down = list(x), list(x)
+        up[n], down[n] = x[n] + 1e-5 * dirn, x[n] - 1e-5 * dirn
+        diff = (loss(*up) - loss(*down)) / 2e-5
+        assert abs(diff - float((want[name] * dirn).sum())) <= 1e-7 * max(1.0, abs(diff))
+
+
+def test_repeats_streams_and_captures():
+    q, k, v, g = (x.to(DEV) for x in make(2, 8, 2, 500, 500, 64, seed=1))
+    lo, hi = (x.to(DEV) for x in documents(2, 500, 4, padding=30))
+    how = dict(scale=0.125, cap=5.0, row_lo=lo, row_hi=hi)
+    O, L = power_attn_exp_fwd(q, k, v, **how)
+    want = [x.clone() for x in (O, L, *power_attn_exp_bwd(q, k, v, O, L, g, **how))]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        O2, L2 = power_attn_exp_fwd(q, k, v, **how)
+        again = O2, L2, *power_attn_exp_bwd(q, k, v, O2, L2, g, **how)
+    side.synchronize()
+    for x, y in zip(again, want):
+        assert torch.equal(x, y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        O3, L3 = power_attn_exp_fwd(q, k, v, **how)
+        held = O3, L3, *power_attn_exp_bwd(q, k, v, O3, L3, g, **how)
+    for n in range(3):
+        for x in held:
+            x.fill_(math.nan)
+        (want[0].float() * n).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(held, want):
+            assert torch.equal(x, y), n
+
+
+def test_offsets_beyond_32_bits():
+    """2^25 keys of 128 channels, of which the last are seen; the rest is whatever memory holds."""
+    T, Tk, d, window = 3, 2 ** 25 + 5, 128, 70
+    q, k, v, g = (x.to(DEV) for x in make(1, 1, 1, T, 200, d, seed=3))
+    K, V = (torch.full((1, 1, Tk, d), math.nan, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    K[:, :, -200:], V[:, :, -200:] = k, v
+    how = dict(scale=d ** -0.5, window=window)
+    want = exp_attn(q.cpu(), k.cpu(), v.cpu(), g=g.cpu(), **how)
+    O, L = power_attn_exp_fwd(q, K, V, **how)
+    dQ, dK, dV = power_attn_exp_bwd(q, K, V, O, L, g, **how)
+    assert not dK[:, :, :-200].any() and not dV[:, :, :-200].any()
+    got = dict(zip(("O", "L", "dQ", "dK", "dV"), (x.float().cpu() for x in (O, L, dQ, dK[:, :, -200:], dV[:, :, -200:]))))
+    check(got, want)
