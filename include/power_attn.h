@@ -249,7 +249,7 @@ pa_status power_attn_exp_bwd(const pa_exp_problem* prob, const void* Q, const vo
  * What exponential attention decodes from, as the power attention's decode state is for it, but growing: tokens are held in
  * pages of a pool that the caller owns, and sequence b finds position t in page table[b][t / page].  A pool holds all key heads
  * of one layer in an order of its own, as bf16 or in 4 bits: per token, key head and 32 channels the minimum m and the unit
- * u = (max - min) / 15 as fp16 and 32 codes c, x = u c + m.  (Computed from the values limited to +-65024, so that every x lies in
+ * u = (max - min) (1 / 15) as fp16 and 32 codes c, x = u c + m.  (Computed from the values limited to +-65024, so that every x lies in
  * the range of fp16, in float32; u and m rounded to nearest, c the nearest integer to (x - m) / u within 0 .. 15, ties to even; 0 where u is 0.  A group
  * with a NaN in it reads back as NaN.)
  * pool: DEVICE, power_attn_cache_bytes() bytes, 16-byte aligned, needs no initialisation.  table: DEVICE int32 [B, max_pages];

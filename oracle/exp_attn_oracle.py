@@ -1,12 +1,14 @@
 """Exponential attention in float64 on the CPU, straight from the definition, with bounds on what float32 arithmetic and bf16
 roundings may change: test infrastructure, no code shared with the library.
 
-Bounds, element by element.  A rounding to bf16 is off by at most U = 2^-8 of the value.  The library rounds the weights P (the
-denominator sums the rounded ones), the gradients t of the products, the results, and D = dO.O is formed from the rounded O.  With ds
-the error of a score in float32 (products exact, d additions, a few operations of the score, at the size of the numbers that enter):
-    |dO_i|  <= U |O_i| + sum_j P_ij (U + 2 ds_ij) |v_j - O_i|                        =: eO_i
+Bounds, element by element.  A rounding to bf16 is off by at most U = 2^-8 of the value.  The library rounds the weights P that
+multiply v (not those that the denominator sums), the gradients t of the products, the results, and D = dO.O is formed from the rounded O.
+With ds the error of a score in float32 (products exact, d additions, a few operations of the score, at the size of the numbers that
+enter) and n the number of keys, whose weights are added in float32:
+    dL_i    <= sum_j P_ij ds_ij + n 2^-24
+    |dO_i|  <= U |O_i| + sum_j P_ij (U + ds_ij + dL_i) |v_j|                          =: eO_i
     |dD_i|  <= sum_c |dO_ic| eO_ic
-    |dP_ij| <= P_ij (ds_ij + dL_i),   dL_i = sum_j P_ij (U + 2 ds_ij), U only as far as the weights it averages over are rounded
+    |dP_ij| <= P_ij (ds_ij + dL_i)
     |dt_ij| <= |t_ij| (U + ds_ij + dL_i) + P_ij (dD_i + 2^-20 |dO_i|.|v_j|)
 and each gradient's sums weigh those, plus U of the result."""
 import math
@@ -64,12 +66,10 @@ def exp_attn(q, k, v, scale=1.0, cap=0.0, window=0, slopes=None, lo=None, hi=Non
             P = torch.where(see, torch.exp(s - torch.where(some, L, 0.0)[:, None]), 0.0)
             ds = torch.where(see, ds + 2.0 ** -21 * (1.0 + torch.where(see, s, 0.0).abs()), 0.0)
             O = P @ vv
-            dev = (vv[None] - O[:, None]).abs()                                        # [T, Tk, d]
-            eO = U * O.abs() + torch.einsum("ij,ijc->ic", P * (U + 2 * ds), dev) + 1e-30
+            dL = (P * ds).sum(1) + Tk * 2.0 ** -24
+            eO = U * O.abs() + (P * (U + ds + dL[:, None])) @ vv.abs() + 1e-30
             if held:
                 eO = eO + P @ (held * vv.abs() + 2.0 ** -24)
-            # the rounding errors of a row's weights are independent, but a short row's may all point one way
-            dL = (P * (U + 2 * ds)).sum(1)
             out["O"][b, h], out["eO"][b, h] = O, eO
             out["L"][b, h] = torch.where(some, L, -math.inf)
             out["eL"][b, h] = dL + 2.0 ** -21 * torch.where(some, L, 0.0).abs()
@@ -112,6 +112,6 @@ def held4(x):
     nan = g.isnan().any(-1, keepdim=True)
     g = g.clamp(-65024.0, 65024.0)
     low, high = g.amin(-1, keepdim=True), g.amax(-1, keepdim=True)
-    unit, low = ((high - low) / torch.full_like(low, 15.0)).half().float(), low.half().float()
+    unit, low = ((high - low) * torch.full_like(low, 1.0 / 15.0)).half().float(), low.half().float()
     code = torch.where(unit > 0, ((g - low) / torch.where(unit > 0, unit, 1.0)).round().clamp(0, 15), 0.0)
     return torch.where(nan, math.nan, code * unit + low).reshape(x.shape)

@@ -130,7 +130,7 @@ __device__ __forceinline__ void hold8(Held& to, const float (&x)[8]) {
     hi = fmaxf(hi, quad<0xB1>(hi));
     lo = least(lo, quad<0x4E>(lo));
     hi = fmaxf(hi, quad<0x4E>(hi));
-    to.unit = (float)(_Float16)((hi - lo) / 15.f);
+    to.unit = (float)(_Float16)((hi - lo) * (1.f / 15.f));
     to.least = (float)(_Float16)lo;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -697,9 +697,10 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
         vec p;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if constexpr (BITS == 16) p[e] = (__bf16)__builtin_amdgcn_exp2f(x[e] - by);
-            else p[e] = (_Float16)__builtin_amdgcn_exp2f(x[e] - by);
-            lsum += (float)p[e];        // the weights that the products use
+            const float y = __builtin_amdgcn_exp2f(x[e] - by);
+            lsum += y;          // (unrounded: L is a result)
+            if constexpr (BITS == 16) p[e] = (__bf16)y;
+            else p[e] = (_Float16)y;
         }
         if (EDGE) vv.keep(slots);
 #pragma unroll

@@ -89,27 +89,109 @@ __device__ __forceinline__ Ends wave_ends(Range r) {
     return e;
 }
 
+// ---- the streamed tile ------------------------------------------------------------------------------------
+// 64 rows, moved from memory to LDS without a register on the way: 16 bytes a lane, so 1 KB of a wave's rows lies one behind the
+// other in LDS.  Two things keep the rows that one cycle of a read touches on different banks: each such KB starts 16 bytes further,
+// and inside it a row's 16-byte pieces are permuted by the row's number.  The permutation leaves enough address bits alone
+// that all of a lane's reads are a few addresses, formed once, and constants.
+template <int HD>
+struct Tile {
+    static constexpr int PIECES = HD / 8, RUN = 512 / HD, STEP = 1040, BYTES = AT / RUN * STEP;     // rows of a KB; their distance
+    static constexpr int NROW = HD == 32 ? 2 : 4, NCOL = HD == 128 ? 4 : 2;
+    uint4 at[BYTES / 16];
+    static __device__ __forceinline__ int turn(int row) {
+        return HD == 128 ? (row & 3) << 2 : HD == 64 ? (row >> 1 & 3) << 1 : (row >> 2 & 1) << 1 | (row >> 3 & 1);
+    }
+    // byte of piece `piece` of a row
+    static __device__ __forceinline__ uint32_t place(int row, int piece) {
+        return (uint32_t)(row / RUN * STEP + row % RUN * 2 * HD + (piece ^ turn(row)) * 16);
+    }
+};
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+// rows row0 .. row0 + 63 of a head of T rows (those past its end as its last one) into a tile; tile_arrived() before the barrier after
+// which they are read.  (Inline, since the compiler would make every LDS read wait for it.)
+template <int HD>
+__device__ __forceinline__ void tile_load(const Tile<HD>& t, const bf16_t* __restrict__ head, int row0, int T, int lane, int w) {
+    using TL = Tile<HD>;
+    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(t.at));
+    const uint64_t from = (uint64_t)(head + (size_t)row0 * HD);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)from), hi = __builtin_amdgcn_readfirstlane((uint32_t)(from >> 32));
+    const uint64_t tile0 = (uint64_t)hi << 32 | lo;
+    const int last = T - 1 - row0, row = lane / TL::PIECES;
+    const uint32_t piece = (uint32_t)(lane % TL::PIECES ^ TL::turn(row)) * 16;      // (turn() is the same in every KB)
+#pragma unroll
+    for (int q = 0; q < HD / 32; ++q) {
+        const int run = 4 * q + w;
+        const uint32_t off = (uint32_t)min(run * TL::RUN + row, last) * (2 * HD) + piece;
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(tile0), "s"(base + run * TL::STEP)
+                     : "memory", "m0");
+    }
+}
+__device__ __forceinline__ void tile_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// A lane's addresses in a tile
+template <int HD>
+struct Reads {
+    uint32_t row[Tile<HD>::NROW], col[Tile<HD>::NCOL];
+    __device__ __forceinline__ explicit Reads(int lane) {
+        const int r16 = lane & 15, h = lane >> 5, odd = lane >> 4 & 1;
+#pragma unroll
+        for (int x = 0; x < Tile<HD>::NROW; ++x) row[x] = Tile<HD>::place(lane & 31, (HD == 128 ? 4 : 2) * x + h);
+#pragma unroll
+        for (int x = 0; x < Tile<HD>::NCOL; ++x)
+            col[x] = Tile<HD>::place(4 * h + (r16 >> 2) + (HD == 32 ? 8 * x : 0), (HD == 32 ? 0 : 4 * x) + 2 * odd + (r16 >> 1 & 1)) + 8 * (r16 & 1);
+    }
+};
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+// rows 32 blk + r32, features 16 ks + 8 h .. + 7 (A or B operand of a contraction over the features); tile: its address
+template <int HD>
+__device__ __forceinline__ bf16x8 row_op(uint32_t tile, const Reads<HD>& rd, int blk, int ks) {
+    Frag f;
+    const uint32_t at = tile + rd.row[HD == 128 ? ks >> 1 : ks] + (HD == 128 ? 32 * (ks & 1) : 0) + blk * (32 / Tile<HD>::RUN * Tile<HD>::STEP);
+    f.q = *(const lds_u32x4*)(uintptr_t)at;
+    return f.v;
+}
+// column 32 cb + r32, k-slots rows 16 j + 4 h .. + 3 and 8 further (A operand of a contraction over the rows), as col_frag in attn_tile.hpp
+template <int HD>
+__device__ __forceinline__ bf16x8 col_op(uint32_t tile, const Reads<HD>& rd, int j, int cb) {
+    constexpr int STEP = Tile<HD>::STEP, RUN = Tile<HD>::RUN;
+    const uint32_t at = tile + rd.col[HD == 32 ? 0 : cb] + j * (16 / RUN * STEP);
+    const uint32_t at8 = HD == 32 ? tile + rd.col[1] + j * STEP : at + 8 / RUN * STEP;
+    union {
+        bf16x8 v;
+        bf16x4 h[2];
+    } f;
+    f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)at);
+    f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(uintptr_t)at8);
+    return f.v;
+}
+
 // Infinities and NaN of rows that are masked for some row of the other side must not reach it, and in a matrix product they would
-// (0 x NaN).  So in tiles that are not seen whole by the whole workgroup such values enter LDS as zeros and their tile row is
-// marked; a wave that finds a mark adds what the pairs that are seen would have received.
+// (0 x NaN).  So in tiles that are not seen whole by the whole workgroup such values are replaced by zeros.  Where there
+// were any, a second walk over those tiles adds what the pairs that are seen would have received.
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t u) { return ((u & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ __forceinline__ bool nonfinite8(uint4 u) {
     return (nonfinite2(u.x) | nonfinite2(u.y) | nonfinite2(u.z) | nonfinite2(u.w)) != 0;
 }
 __device__ __forceinline__ uint32_t finite2(uint32_t u) { return u & ~((nonfinite2(u) >> 15) * 0xffffu); }
-struct Marks {
-    uint32_t row[3][2];     // of the tile in use, the one being staged, and the one cleared for the next
-};
-__device__ __forceinline__ void clean(uint4& u, uint32_t (&marks)[2], int row) {
-    if (!nonfinite8(u)) return;
-    u = make_uint4(finite2(u.x), finite2(u.y), finite2(u.z), finite2(u.w));
-    atomicOr(&marks[row >> 5], 1u << (row & 31));
+template <int HD>
+__device__ __forceinline__ void tile_clean(Tile<HD>& t, int& found, int tid) {
+    const int lane = tid & 63, w = tid >> 6;
+#pragma unroll
+    for (int q = 0; q < HD / 32; ++q) {
+        uint4* at = &t.at[(4 * q + w) * (Tile<HD>::STEP / 16) + lane];
+        const uint4 u = *at;
+        if (!nonfinite8(u)) continue;
+        *at = make_uint4(finite2(u.x), finite2(u.y), finite2(u.z), finite2(u.w));
+        found = 1;
+    }
 }
-#define PA_TILE_CLEAN(REGS, MARKS) \
-    _Pragma("unroll") for (int q_ = 0; q_ < HD / 32; ++q_) clean(REGS[q_], MARKS, (tid + 256 * q_) / (HD / 8));
-__device__ __forceinline__ uint64_t marked(const uint32_t (&m)[2]) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)m[0]) |
-           (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)m[1]) << 32;
+// whether a row of HD values (at `row`, in memory) has an infinity or a NaN among them; the same for the whole wave
+template <int HD>
+__device__ __forceinline__ bool row_nonfinite(const bf16_t* __restrict__ row, int lane) {
+    return __any(nonfinite8(*(const uint4*)(row + 8 * (lane % (HD / 8)))));
 }
 
 // ---- the order of the workgroups ------------------------------------------------------------------------
@@ -139,9 +221,9 @@ __device__ __forceinline__ bool place(const Order& o, Place& p) {
 // and most tiles then rescale nothing).
 template <int HD>
 struct FwdShared {
-    AttnTile<HD> k[2], v[2];
+    Tile<HD> k[2], v[2];
     Ends ends[4];
-    Marks marks;
+    int found;       // infinities or NaN in a tile that is not seen whole
 };
 template <int HD, int OWN, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
@@ -180,13 +262,14 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
     const float slope = BIAS ? slopes[head - b * order.H] * LOG2E : 0.f;
 
     if (lane == 0) sm.ends[w] = mine;
-    if (tid < 6) (&sm.marks.row[0][0])[tid] = 0;
+    if (tid == 0) sm.found = 0;
     __syncthreads();
     Ends all = join(join(sm.ends[0], sm.ends[1]), join(sm.ends[2], sm.ends[3]));
     const int t_lo = __builtin_amdgcn_readfirstlane(all.lo_min) / AT, t_hi = (__builtin_amdgcn_readfirstlane(all.hi_max) + AT - 1) / AT;
 
-    auto tile = [&](auto mask_c, int buf, int key0, uint64_t bad) {
-        constexpr bool MASK = decltype(mask_c)::value;
+    const Reads<HD> rd(lane);
+    auto tile = [&](int buf, int key0, bool masked) {
+        const uint32_t kt = lds_address(sm.k[0].at) + buf * Tile<HD>::BYTES, vt = kt + 2 * Tile<HD>::BYTES;
         f32x16 c[2][NI];        // S^T: key 32 kb + 8 k + 4 h + r, query 32 ib + r32
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -194,7 +277,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
             for (int ib = 0; ib < NI; ++ib) c[kb][ib] = splat16(0.f);
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks) {
-                const bf16x8 kf = row_frag<HD>(sm.k[buf], kb, ks, lane);
+                const bf16x8 kf = row_op<HD>(kt, rd, kb, ks);
 #pragma unroll
                 for (int ib = 0; ib < NI; ++ib) c[kb][ib] = mfma32(kf, qf[ib][ks], c[kb][ib]);
             }
@@ -203,20 +286,30 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
 #pragma unroll
         for (int ib = 0; ib < NI; ++ib) {
             const float far = BIAS ? (float)(q0 + 32 * ib + r32 + rows.off - key0 - 4 * h) : 0.f;
+            if (!RAW)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x = c[kb][ib][i];
+                        if (CAP) x = fmaf(-2.f * sc.capl, cap_r(x, sc), sc.capl);
+                        else x *= sc.sl;
+                        if (BIAS) x = fmaf(-slope, fabsf(far - (float)(32 * kb + 8 * (i >> 2) + (i & 3))), x);
+                        c[kb][ib][i] = x;
+                    }
+            if (masked) {
+                const int key = key0 + 4 * h - rg[ib].lo, n = max(rg[ib].hi - rg[ib].lo, 0);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if ((unsigned)(key + 32 * kb + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) c[kb][ib][i] = NEG_INF;
+            }
             float top[2] = {NEG_INF, NEG_INF};
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = 32 * kb + 8 * (i >> 2) + (i & 3);       // of the tile, less 4 h
-                    float x = c[kb][ib][i];
-                    if (CAP) x = fmaf(-2.f * sc.capl, cap_r(x, sc), sc.capl);
-                    else if (BIAS) x *= sc.sl;
-                    if (BIAS) x = fmaf(-slope, fabsf(far - (float)key), x);
-                    if (MASK && !sees(key0 + 4 * h + key, rg[ib])) x = NEG_INF;
-                    c[kb][ib][i] = x;
-                    top[kb] = fmaxf(top[kb], x);
-                }
+                for (int i = 0; i < 16; ++i) top[kb] = fmaxf(top[kb], c[kb][ib][i]);
             float lo, hi;
             halves(fmaxf(top[0], top[1]), lo, hi);
             const float t = RAW ? fmaxf(lo, hi) * sc.sl : fmaxf(lo, hi);
@@ -239,69 +332,64 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
             for (int ib = 0; ib < NI; ++ib) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float x = c[kb][ib][i];
-                    pf[ib][i >> 3].v[i & 7] = (__bf16)__builtin_amdgcn_exp2f(RAW ? fmaf(x, sc.sl, -mm[ib]) : x - mm[ib]);
+                    const float x = c[kb][ib][i], p = __builtin_amdgcn_exp2f(RAW ? fmaf(x, sc.sl, -mm[ib]) : x - mm[ib]);
+                    lsum[ib] += p;      // (unrounded: L is a result)
+                    pf[ib][i >> 3].v[i & 7] = (__bf16)p;
                 }
-                // the denominator sums the rounded weights, the ones that the numerator uses
-#pragma unroll
-                for (int j = 0; j < 2; ++j) lsum[ib] = sum_bf16x8(pf[ib][j], lsum[ib]);
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int vb = 0; vb < NV; ++vb) {
-                    const bf16x8 vf = col_frag<HD>(sm.v[buf], 2 * kb + j, vb, lane);
+                    const bf16x8 vf = col_op<HD>(vt, rd, 2 * kb + j, vb);
 #pragma unroll
                     for (int ib = 0; ib < NI; ++ib) acc[vb][ib] = mfma32(vf, pf[ib][j].v, acc[vb][ib]);
                 }
         }
-        for (; bad != 0; bad &= bad - 1) {      // values that entered as zeros
-            const int key = key0 + __builtin_ctzll(bad);
-            const bf16_t* v = Vh + (size_t)min(key, T - 1) * HD;
+    };
+
+    if (t_lo < t_hi) {
+        tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
+        tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
+    }
+    tile_arrived();
+    __syncthreads();
+    for (int t = t_lo; t < t_hi; ++t) {
+        const int buf = (t - t_lo) & 1, key0 = t * AT;
+        if (t + 1 < t_hi) {
+            tile_load(sm.k[buf ^ 1], Kh, key0 + AT, T, lane, w);
+            tile_load(sm.v[buf ^ 1], Vh, key0 + AT, T, lane, w);
+        }
+        if (!all.all(key0, AT)) {
+            tile_clean(sm.v[buf], sm.found, tid);
+            lds_barrier();
+        }
+        if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
+        tile_arrived();
+        __syncthreads();
+    }
+
+    if (sm.found != 0) {     // the values that entered as zeros
+        for (int t = t_lo; t < t_hi; ++t) {
+            if (all.all(t * AT, AT) || mine.none(t * AT, AT)) continue;
+            for (int key = t * AT; key < min(t * AT + AT, T); ++key) {
+                bool any = false;
 #pragma unroll
-            for (int ib = 0; ib < NI; ++ib)
-                if (sees(key, rg[ib]))
+                for (int ib = 0; ib < NI; ++ib) any |= sees(key, rg[ib]);
+                const bf16_t* v = Vh + (size_t)key * HD;
+                if (!__any(any) || !row_nonfinite<HD>(v, lane)) continue;
+#pragma unroll
+                for (int ib = 0; ib < NI; ++ib)
 #pragma unroll
                     for (int vb = 0; vb < NV; ++vb)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const uint32_t u = v[32 * vb + 8 * (i >> 2) + 4 * h + (i & 3)];
-                            if (nonfinite2(u) != 0) acc[vb][ib][i] += __uint_as_float(u << 16);
+                            if (nonfinite2(u) != 0 && sees(key, rg[ib])) acc[vb][ib][i] += __uint_as_float(u << 16);
                         }
+            }
         }
-    };
-
-    uint4 kr[HD / 32], vr[HD / 32];
-    if (t_lo < t_hi) {
-        PA_TILE_LOAD(kr, Kh, t_lo * AT, false)
-        PA_TILE_LOAD(vr, Vh, t_lo * AT, false)
-        if (!all.all(t_lo * AT, AT)) PA_TILE_CLEAN(vr, sm.marks.row[0])
-        PA_TILE_STORE(sm.k[0], kr)
-        PA_TILE_STORE(sm.v[0], vr)
     }
-    __syncthreads();
-    int slot = 0;
-    for (int t = t_lo; t < t_hi; ++t) {
-        const int buf = (t - t_lo) & 1, key0 = t * AT, next = slot == 2 ? 0 : slot + 1;
-        if (t + 1 < t_hi) {
-            PA_TILE_LOAD(kr, Kh, key0 + AT, false)
-            PA_TILE_LOAD(vr, Vh, key0 + AT, false)
-        }
-        if (!mine.none(key0, AT)) {
-            const uint64_t bad = all.all(key0, AT) ? 0 : marked(sm.marks.row[slot]);
-            if (mine.all(key0, AT)) tile(std::false_type{}, buf, key0, bad);
-            else tile(std::true_type{}, buf, key0, bad);
-        }
-        if (t + 1 < t_hi) {
-            if (!all.all(key0 + AT, AT)) PA_TILE_CLEAN(vr, sm.marks.row[next])
-            PA_TILE_STORE(sm.k[buf ^ 1], kr)
-            PA_TILE_STORE(sm.v[buf ^ 1], vr)
-        }
-        if (tid < 2) sm.marks.row[next == 2 ? 0 : next + 1][tid] = 0;   // read last one tile ago, marked next one tile on
-        slot = next;
-        __syncthreads();
-    }
-
 #pragma unroll
     for (int ib = 0; ib < NI; ++ib) {
         const int i = q0 + 32 * ib + r32;
@@ -408,13 +496,14 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
     const float slope = BIAS ? slopes[head - b * order.H] * LOG2E : 0.f;
 
     if (lane == 0) sm.ends[w] = mine;
-    if (tid < 6) (&sm.marks.row[0][0])[tid] = 0;
+    if (tid == 0) sm.found = 0;
     __syncthreads();
     Ends all = join(join(sm.ends[0], sm.ends[1]), join(sm.ends[2], sm.ends[3]));
     const int t_lo = __builtin_amdgcn_readfirstlane(all.lo_min) / AT, t_hi = (__builtin_amdgcn_readfirstlane(all.hi_max) + AT - 1) / AT;
 
-    auto tile = [&](auto mask_c, int buf, int key0, uint64_t bad) {
-        constexpr bool MASK = decltype(mask_c)::value;
+    const Reads<HD> rd(lane);
+    auto tile = [&](int buf, int key0, bool masked) {
+        const uint32_t kt = lds_address(sm.k[0].at) + buf * Tile<HD>::BYTES, vt = kt + 2 * Tile<HD>::BYTES;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             f32x16 c[NI], e[NI];        // S^T and (dO V^T - D)^T: key 32 kb + 8 k + 4 h + r, query 32 ib + r32
@@ -425,7 +514,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
             }
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks) {
-                const bf16x8 kf = row_frag<HD>(sm.k[buf], kb, ks, lane), vf = row_frag<HD>(sm.v[buf], kb, ks, lane);
+                const bf16x8 kf = row_op<HD>(kt, rd, kb, ks), vf = row_op<HD>(vt, rd, kb, ks);
 #pragma unroll
                 for (int ib = 0; ib < NI; ++ib) {
                     c[ib] = mfma32(kf, qf[ib][ks], c[ib]);
@@ -442,60 +531,65 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
                     const int key = 8 * (i >> 2) + (i & 3);
                     float p, t;
                     pair_grad<CAP, BIAS>(c[ib][i], e[ib][i], st[ib].x, slope, far - (float)key, sc, p, t);
-                    if (MASK && !sees(key0 + 32 * kb + 4 * h + key, rg[ib])) t = 0.f;
-                    tf[ib][i >> 3].v[i & 7] = (__bf16)t;
+                    e[ib][i] = t;
                 }
+                if (masked) {
+                    const int key = key0 + 32 * kb + 4 * h - rg[ib].lo, n = max(rg[ib].hi - rg[ib].lo, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if ((unsigned)(key + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) e[ib][i] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) tf[ib][i >> 3].v[i & 7] = (__bf16)e[ib][i];
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int fb = 0; fb < NF; ++fb) {
-                    const bf16x8 kc = col_frag<HD>(sm.k[buf], 2 * kb + j, fb, lane);   // K^T
+                    const bf16x8 kc = col_op<HD>(kt, rd, 2 * kb + j, fb);   // K^T
 #pragma unroll
                     for (int ib = 0; ib < NI; ++ib) acc[fb][ib] = mfma32(kc, tf[ib][j].v, acc[fb][ib]);
                 }
         }
-        for (; bad != 0; bad &= bad - 1) {      // a key that is no finite vector: nothing is left of the rows that see it
-            const int key = key0 + __builtin_ctzll(bad);
-#pragma unroll
-            for (int ib = 0; ib < NI; ++ib)
-                if (sees(key, rg[ib]))
-#pragma unroll
-                    for (int fb = 0; fb < NF; ++fb) acc[fb][ib] = splat16(__builtin_nanf(""));
-        }
     };
 
-    uint4 kr[HD / 32], vr[HD / 32];
     if (t_lo < t_hi) {
-        PA_TILE_LOAD(kr, Kh, t_lo * AT, false)
-        PA_TILE_LOAD(vr, Vh, t_lo * AT, false)
-        if (!all.all(t_lo * AT, AT)) PA_TILE_CLEAN(kr, sm.marks.row[0])
-        PA_TILE_STORE(sm.k[0], kr)
-        PA_TILE_STORE(sm.v[0], vr)
+        tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
+        tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
     }
+    tile_arrived();
     __syncthreads();
-    int slot = 0;
     for (int t = t_lo; t < t_hi; ++t) {
-        const int buf = (t - t_lo) & 1, key0 = t * AT, next = slot == 2 ? 0 : slot + 1;
+        const int buf = (t - t_lo) & 1, key0 = t * AT;
         if (t + 1 < t_hi) {
-            PA_TILE_LOAD(kr, Kh, key0 + AT, false)
-            PA_TILE_LOAD(vr, Vh, key0 + AT, false)
+            tile_load(sm.k[buf ^ 1], Kh, key0 + AT, T, lane, w);
+            tile_load(sm.v[buf ^ 1], Vh, key0 + AT, T, lane, w);
         }
-        if (!mine.none(key0, AT)) {
-            const uint64_t bad = all.all(key0, AT) ? 0 : marked(sm.marks.row[slot]);
-            if (mine.all(key0, AT)) tile(std::false_type{}, buf, key0, bad);
-            else tile(std::true_type{}, buf, key0, bad);
+        if (!all.all(key0, AT)) {
+            tile_clean(sm.k[buf], sm.found, tid);
+            lds_barrier();
         }
-        if (t + 1 < t_hi) {
-            if (!all.all(key0 + AT, AT)) PA_TILE_CLEAN(kr, sm.marks.row[next])
-            PA_TILE_STORE(sm.k[buf ^ 1], kr)
-            PA_TILE_STORE(sm.v[buf ^ 1], vr)
-        }
-        if (tid < 2) sm.marks.row[next == 2 ? 0 : next + 1][tid] = 0;
-        slot = next;
+        if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
+        tile_arrived();
         __syncthreads();
     }
 
+    if (sm.found != 0) {     // nothing is left of the rows that see a key that is no finite vector
+        for (int t = t_lo; t < t_hi; ++t) {
+            if (all.all(t * AT, AT) || mine.none(t * AT, AT)) continue;
+            for (int key = t * AT; key < min(t * AT + AT, T); ++key) {
+                bool any = false;
+#pragma unroll
+                for (int ib = 0; ib < NI; ++ib) any |= sees(key, rg[ib]);
+                if (!__any(any) || !row_nonfinite<HD>(Kh + (size_t)key * HD, lane)) continue;
+#pragma unroll
+                for (int ib = 0; ib < NI; ++ib)
+                    if (sees(key, rg[ib]))
+#pragma unroll
+                        for (int fb = 0; fb < NF; ++fb) acc[fb][ib] = splat16(__builtin_nanf(""));
+            }
+        }
+    }
 #pragma unroll
     for (int ib = 0; ib < NI; ++ib) {
         const int i = q0 + 32 * ib + r32;
@@ -511,10 +605,10 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
 // ends that the preparation left.
 template <int HD>
 struct BwdShared {
-    AttnTile<HD> q[2], g[2];
+    Tile<HD> q[2], g[2];
     float l2[2][AT], d[2][AT];
     int lo[2][AT], hi[2][AT];
-    Marks marks;
+    int found;
 };
 template <int HD, int OWN, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
@@ -549,11 +643,12 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
             dv[fb][kb] = splat16(0.f);
         }
     }
-    if (tid < 6) (&sm.marks.row[0][0])[tid] = 0;
+    if (tid == 0) sm.found = 0;
     __syncthreads();
 
-    auto tile = [&](auto mask_c, int buf, int q0, float slope, uint64_t bad) {
-        constexpr bool MASK = decltype(mask_c)::value;
+    const Reads<HD> rd(lane);
+    auto tile = [&](int buf, int q0, float slope, bool masked) {
+        const uint32_t qt = lds_address(sm.q[0].at) + buf * Tile<HD>::BYTES, gt = qt + 2 * Tile<HD>::BYTES;
 #pragma unroll
         for (int qb = 0; qb < 2; ++qb) {
             float l2[16], g0[16];
@@ -568,7 +663,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
             }
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks) {
-                const bf16x8 qa = row_frag<HD>(sm.q[buf], qb, ks, lane), ga = row_frag<HD>(sm.g[buf], qb, ks, lane);
+                const bf16x8 qa = row_op<HD>(qt, rd, qb, ks), ga = row_op<HD>(gt, rd, qb, ks);
 #pragma unroll
                 for (int kb = 0; kb < NJ; ++kb) {
                     c[kb] = mfma32(qa, kf[kb][ks], c[kb]);
@@ -585,35 +680,34 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
                     const int r = 8 * (i >> 2) + (i & 3);
                     float p, t;
                     pair_grad<CAP, BIAS>(c[kb][i], e[kb][i], l2[i], slope, far + (float)r, sc, p, t);
-                    if (MASK) {
-                        const int i_row = 32 * qb + 4 * h + r;
-                        if (!sees(key, {sm.lo[buf][i_row], sm.hi[buf][i_row]})) p = t = 0.f;
+                    c[kb][i] = p;
+                    e[kb][i] = t;
+                }
+                if (masked) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int row = 32 * qb + 4 * h + 8 * (i >> 2) + (i & 3);
+                        if (!sees(key, {sm.lo[buf][row], sm.hi[buf][row]})) c[kb][i] = e[kb][i] = 0.f;
                     }
-                    pf[kb][i >> 3].v[i & 7] = (__bf16)p;
-                    tf[kb][i >> 3].v[i & 7] = (__bf16)t;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    pf[kb][i >> 3].v[i & 7] = (__bf16)c[kb][i];
+                    tf[kb][i >> 3].v[i & 7] = (__bf16)e[kb][i];
                 }
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int fb = 0; fb < NF; ++fb) {
-                    const bf16x8 qc = col_frag<HD>(sm.q[buf], 2 * qb + j, fb, lane);   // Q^T
-                    const bf16x8 gc = col_frag<HD>(sm.g[buf], 2 * qb + j, fb, lane);   // dO^T
+                    const bf16x8 qc = col_op<HD>(qt, rd, 2 * qb + j, fb);   // Q^T
+                    const bf16x8 gc = col_op<HD>(gt, rd, 2 * qb + j, fb);   // dO^T
 #pragma unroll
                     for (int kb = 0; kb < NJ; ++kb) {
                         dk[fb][kb] = mfma32(qc, tf[kb][j].v, dk[fb][kb]);
                         dv[fb][kb] = mfma32(gc, pf[kb][j].v, dv[fb][kb]);
                     }
                 }
-        }
-        for (; bad != 0; bad &= bad - 1) {      // a query or a gradient that is no finite vector
-            const int r = __builtin_ctzll(bad);
-            const Range rg{sm.lo[buf][r], sm.hi[buf][r]};
-#pragma unroll
-            for (int kb = 0; kb < NJ; ++kb)
-                if (sees(k0 + 32 * kb + r32, rg))
-#pragma unroll
-                    for (int fb = 0; fb < NF; ++fb) dk[fb][kb] = dv[fb][kb] = splat16(__builtin_nanf(""));
         }
     };
 
@@ -637,26 +731,19 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
         left &= left - 1;
         return t;
     };
-    uint4 qr[HD / 32], gr[HD / 32];
     float2 str = make_float2(0.f, 0.f);
     int2 rgr = make_int2(0, 0);
-    auto load = [&](int t, int head) {
+    auto load = [&](int t, int head, int buf) {
         const size_t base_row = (size_t)head * T;
-        PA_TILE_LOAD(qr, Q + base_row * HD, t * AT, false)
-        PA_TILE_LOAD(gr, dO + base_row * HD, t * AT, false)
         if (tid < AT) {
             const int i = min(t * AT + tid, T - 1);
             str = from.stat[base_row + i];
             rgr = t * AT + tid < T ? range[i] : make_int2(rows.Tk, 0);
         }
+        tile_load(sm.q[buf], Q + base_row * HD, t * AT, T, lane, w);
+        tile_load(sm.g[buf], dO + base_row * HD, t * AT, T, lane, w);
     };
-    auto store = [&](int buf, uint32_t (&marks)[2], const Ends& e) {
-        if (!e.all(j0, WG)) {
-            PA_TILE_CLEAN(qr, marks)
-            PA_TILE_CLEAN(gr, marks)
-        }
-        PA_TILE_STORE(sm.q[buf], qr)
-        PA_TILE_STORE(sm.g[buf], gr)
+    auto store = [&](int buf) {
         if (tid < AT) {
             sm.l2[buf][tid] = str.x;
             sm.d[buf][tid] = str.y;
@@ -669,37 +756,61 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
         return Ends{__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y), __builtin_amdgcn_readfirstlane(e.z),
                     __builtin_amdgcn_readfirstlane(e.w)};
     };
-    int t = advance(), gt = g, buf = 0, slot = 0;
+    int t = advance(), gt = g, buf = 0;
     Ends e{0, 0, 0, 0};
     if (t >= 0) {
         e = ends_of(t);
-        load(t, head0 + gt);
-        store(0, sm.marks.row[0], e);
+        load(t, head0 + gt, 0);
+        store(0);
     }
+    tile_arrived();
     __syncthreads();
     while (t >= 0) {
-        const int tn = advance(), gn = g, next = slot == 2 ? 0 : slot + 1;
+        const int tn = advance(), gn = g;
         Ends en{0, 0, 0, 0};
         if (tn >= 0) {
             en = ends_of(tn);
-            load(tn, head0 + gn);
+            load(tn, head0 + gn, buf ^ 1);
         }
-        if (!e.none(k0, OWN)) {
-            const float slope = BIAS ? slopes[head0 + gt - b * order.H] * LOG2E : 0.f;
-            const uint64_t bad = e.all(j0, WG) ? 0 : marked(sm.marks.row[slot]);
-            if (e.all(k0, OWN)) tile(std::false_type{}, buf, t * AT, slope, bad);
-            else tile(std::true_type{}, buf, t * AT, slope, bad);
+        if (!e.all(j0, WG)) {
+            tile_clean(sm.q[buf], sm.found, tid);
+            tile_clean(sm.g[buf], sm.found, tid);
+            lds_barrier();
         }
-        if (tn >= 0) store(buf ^ 1, sm.marks.row[next], en);
-        if (tid < 2) sm.marks.row[next == 2 ? 0 : next + 1][tid] = 0;
-        slot = next;
+        if (!e.none(k0, OWN)) tile(buf, t * AT, BIAS ? slopes[head0 + gt - b * order.H] * LOG2E : 0.f, !e.all(k0, OWN));
+        if (tn >= 0) store(buf ^ 1);
         buf ^= 1;
         t = tn;
         gt = gn;
         e = en;
+        tile_arrived();
         __syncthreads();
     }
 
+    if (sm.found != 0) {     // nothing is left of the keys that a row sees whose query or gradient is no finite vector
+        for (int t = 0; t < ntile; ++t) {
+            const Ends e = ends_of(t);
+            if (e.all(j0, WG) || e.none(k0, OWN)) continue;
+            for (int i = t * AT; i < min(t * AT + AT, T); ++i) {
+                const Range rg{range[i].x, range[i].y};
+                bool any = false;
+#pragma unroll
+                for (int kb = 0; kb < NJ; ++kb) any |= sees(k0 + 32 * kb + r32, rg);
+                if (!__any(any)) continue;
+                bool bad = false;
+                for (int g = 0; g < order.G; ++g) {
+                    const size_t row = ((size_t)(head0 + g) * T + i) * HD;
+                    bad |= row_nonfinite<HD>(Q + row, lane) || row_nonfinite<HD>(dO + row, lane);
+                }
+                if (!bad) continue;
+#pragma unroll
+                for (int kb = 0; kb < NJ; ++kb)
+                    if (sees(k0 + 32 * kb + r32, rg))
+#pragma unroll
+                        for (int fb = 0; fb < NF; ++fb) dk[fb][kb] = dv[fb][kb] = splat16(__builtin_nanf(""));
+            }
+        }
+    }
 #pragma unroll
     for (int kb = 0; kb < NJ; ++kb) {
         const int key = k0 + 32 * kb + r32;
