@@ -432,143 +432,117 @@ struct Elem<4> {
 __device__ __forceinline__ f32x4 mfma_step(bf16x8 a, bf16x8 b, f32x4 c) { return mfma16(a, b, c); }
 __device__ __forceinline__ f32x4 mfma_step(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// two codes (nibbles `at` / 4 of both halves) as fp16: 1024 + c has c in its last bits
+// two codes (nibbles AT / 4 of both halves) as fp16: 1024 + c has c in its last bits.  magic: 0x64006400 in a vector register (with a second
+// constant v_and_or_b32 would not be one instruction)
 template <int AT>
-__device__ __forceinline__ f16x2 codes2(uint32_t w) {
+__device__ __forceinline__ f16x2 codes2(uint32_t w, uint32_t magic) {
     union {
         uint32_t u;
         f16x2 h;
     } x;
     if (AT == 0 || AT == 8) {
-        x.u = ((AT == 8 ? w >> 8 : w) & 0x000f000fu) | 0x64006400u;
+        x.u = ((AT == 8 ? w >> 8 : w) & 0x000f000fu) | magic;
         return x.h - (f16x2){1024, 1024};
     }
-    x.u = ((AT == 12 ? w >> 8 : w) & 0x00f000f0u) | 0x64006400u;       // 1024 + 16 c
+    x.u = ((AT == 12 ? w >> 8 : w) & 0x00f000f0u) | magic;       // 1024 + 16 c
     return __builtin_elementwise_fma(x.h, (f16x2){0.0625f, 0.0625f}, (f16x2){-64, -64});
 }
 
-// A unit's operands as they lie in memory, and as the products take them
+// A unit (32 tokens of a key head) in LDS: keys, values, parameters (4 bits; keys' 4 HD bytes, then values'), as they lie in the page
 template <int HD, int BITS>
-struct Keys;
-template <int HD, int BITS>
-struct Values;
-template <int HD>
-struct Keys<HD, 16> {
-    Frag f[2][HD / 32];
-    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
-        const char* p = block + ((size_t)unit * 2 * (HD / 32) * 64 + lane) * 16;
+struct Unit {
+    static constexpr int CODES = UNIT * HD * BITS / 8, BYTES = 2 * CODES + (BITS == 4 ? 1024 : 0), LOADS = BYTES / 1024;
+    // loads of it issued by a wave; block: the page's block of the head, unit: of the page
+    static __device__ __forceinline__ void load(uint32_t lds, uint64_t block, int page, int unit, int lane) {
+        const uint64_t k = block + (uint32_t)(unit * CODES), v = k + Layout<HD, BITS>::values(page);
 #pragma unroll
-        for (int n = 0; n < 2 * (HD / 32); ++n) f[n / (HD / 32)][n % (HD / 32)].u = *(const uint4*)(p + n * 1024);
-    }
-    __device__ __forceinline__ bf16x8 operand(int blk, int ks) const { return f[blk][ks].v; }
-};
-template <int HD>
-struct Values<HD, 16> {
-    Frag f[HD / 16];
-    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
-        const char* p = block + Layout<HD, 16>::values(pg.page) + ((size_t)unit * (HD / 16) * 64 + lane) * 16;
-#pragma unroll
-        for (int n = 0; n < HD / 16; ++n) f[n].u = *(const uint4*)(p + n * 1024);
-    }
-    // slots whose token is not seen hold zeros: their weight is 0, but what memory holds there may be no number
-    __device__ __forceinline__ void keep(uint32_t slots) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (!(slots >> e & 1))
-#pragma unroll
-                for (int n = 0; n < HD / 16; ++n) f[n].v[e] = (__bf16)0.f;
-    }
-    __device__ __forceinline__ bf16x8 operand(int cb) const { return f[cb].v; }
-};
-template <int HD>
-struct Keys<HD, 4> {
-    uint32_t w[2][HD / 32];
-    _Float16 u[2][HD / 32], m[2][HD / 32];
-    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
-        const char* p = block + ((size_t)unit * 2 * 64 + lane) * (HD / 8);
-        const char* q = block + Layout<HD, 4>::k_params(pg.page) + (size_t)(unit * UNIT + lane % 16) * (HD / 8);
-#pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            if constexpr (HD == 128) {
-                const uint4 x = *(const uint4*)(p + blk * 64 * 16);
-                w[blk][0] = x.x; w[blk][1] = x.y; w[blk][2] = x.z; w[blk][3] = x.w;
-                const f16x8 h = *(const f16x8*)(q + blk * 16 * 16);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    u[blk][k] = h[k];
-                    m[blk][k] = h[4 + k];
-                }
-            } else {
-                typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
-                const uint2 x = *(const uint2*)(p + blk * 64 * 8);
-                w[blk][0] = x.x; w[blk][1] = x.y;
-                const f16x4 h = *(const f16x4*)(q + blk * 16 * 8);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    u[blk][k] = h[k];
-                    m[blk][k] = h[2 + k];
-                }
-            }
+        for (int i = 0; i < CODES / 1024; ++i) {
+            dma16(k + i * 1024, lane * 16, lds + i * 1024);
+            dma16(v + i * 1024, lane * 16, lds + CODES + i * 1024);
+        }
+        if constexpr (BITS == 4) {
+            constexpr int N = HD / 4;       // lanes that the keys' parameters take, and the values'
+            const uint32_t off = lane < N ? (uint32_t)Layout<HD, 4>::k_params(page) + lane * 16
+                                          : (uint32_t)Layout<HD, 4>::v_params(page) + min(lane - N, N - 1) * 16;
+            dma16(block + (uint32_t)(unit * 4 * HD), off, lds + 2 * CODES);
         }
     }
-    __device__ __forceinline__ f16x8 operand(int blk, int ks) const {
-        const f16x2 u2 = {u[blk][ks], u[blk][ks]}, m2 = {m[blk][ks], m[blk][ks]};
-        const uint32_t x = w[blk][ks];
-        union {
-            f16x2 h[4];
-            f16x8 v;
-        } o;
-        o.h[0] = __builtin_elementwise_fma(codes2<0>(x), u2, m2);
-        o.h[1] = __builtin_elementwise_fma(codes2<4>(x), u2, m2);
-        o.h[2] = __builtin_elementwise_fma(codes2<8>(x), u2, m2);
-        o.h[3] = __builtin_elementwise_fma(codes2<12>(x), u2, m2);
-        return o.v;
+    static __device__ __forceinline__ Frag piece(uint32_t at) {
+        Frag f;
+        f.q = *(const lds_u32x4*)(uintptr_t)at;
+        return f;
     }
+    // Slots (of this lane's group) whose token is not seen get zeros: their weight is 0, but what memory holds there may be no number.
+    static __device__ __forceinline__ void keep(uint32_t lds, uint32_t slots, int lane) {
+        auto zero = [&](uint32_t at, uint32_t keep) {
+            u32x4 x = *(lds_u32x4*)(uintptr_t)at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] &= (keep >> (2 * i) & 1 ? 0xffffu : 0u) | (keep >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
+            *(lds_u32x4*)(uintptr_t)at = x;
+        };
+        if constexpr (BITS == 16) {
+#pragma unroll
+            for (int cb = 0; cb < HD / 16; ++cb) zero(lds + CODES + cb * 1024 + lane * 16, slots);
+        } else {        // the parameters: [channel / 32][lane group][unit, minimum] of 16 bytes
+            const uint32_t of = __shfl(slots, lane / 2 % 4 * 16);
+            if (lane < HD / 4) zero(lds + 2 * CODES + 4 * HD + lane * 16, of);
+        }
+    }
+};
+// operands of the two products
+template <int HD>
+__device__ __forceinline__ bf16x8 key_op(std::integral_constant<int, 16>, uint32_t lds, int blk, int ks, int lane, uint32_t) {
+    return Unit<HD, 16>::piece(lds + (blk * (HD / 32) + ks) * 1024 + lane * 16).v;
+}
+template <int HD>
+__device__ __forceinline__ void value_ops(std::integral_constant<int, 16>, bf16x8 (&op)[2], uint32_t lds, int cg, int lane, uint32_t) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n) op[n] = Unit<HD, 16>::piece(lds + Unit<HD, 16>::CODES + (2 * cg + n) * 1024 + lane * 16).v;
+}
+union Half8 {
+    u32x4 q;
+    f16x8 v;
+    f16x2 h[4];
 };
 template <int HD>
-struct Values<HD, 4> {
-    uint4 c[HD / 64];
-    f16x8 u[HD / 32], m[HD / 32];
-    __device__ __forceinline__ void load(const char* block, const Pages& pg, int unit, int lane) {
-        const char* p = block + Layout<HD, 4>::values(pg.page) + ((size_t)unit * (HD / 64) * 64 + lane) * 16;
-        const char* q = block + Layout<HD, 4>::v_params(pg.page) + ((size_t)unit * (HD / 32) * 4 + lane / 16) * 32;
+__device__ __forceinline__ void key_ops4(f16x8 (&op)[HD / 32], uint32_t lds, int blk, int lane, uint32_t magic) {
+    constexpr int NK = HD / 32;
+    typedef __attribute__((ext_vector_type(NK))) uint32_t words;
+    using LP = __attribute__((address_space(3))) const words*;
+    const words w = *(LP)(uintptr_t)(lds + blk * (Unit<HD, 4>::CODES / 2) + lane * (HD / 8));
+    union {
+        words u;
+        _Float16 h[2 * NK];
+    } par;
+    par.u = *(LP)(uintptr_t)(lds + 2 * Unit<HD, 4>::CODES + (16 * blk + lane % 16) * (HD / 8));
 #pragma unroll
-        for (int n = 0; n < HD / 64; ++n) c[n] = *(const uint4*)(p + n * 1024);
-#pragma unroll
-        for (int n = 0; n < HD / 32; ++n) {
-            u[n] = *(const f16x8*)(q + n * 128);
-            m[n] = *(const f16x8*)(q + n * 128 + 16);
-        }
+    for (int ks = 0; ks < NK; ++ks) {
+        const f16x2 u = {par.h[ks], par.h[ks]}, m = {par.h[NK + ks], par.h[NK + ks]};
+        Half8 o;
+        o.h[0] = __builtin_elementwise_fma(codes2<0>(w[ks], magic), u, m);
+        o.h[1] = __builtin_elementwise_fma(codes2<4>(w[ks], magic), u, m);
+        o.h[2] = __builtin_elementwise_fma(codes2<8>(w[ks], magic), u, m);
+        o.h[3] = __builtin_elementwise_fma(codes2<12>(w[ks], magic), u, m);
+        op[ks] = o.v;
     }
-    __device__ __forceinline__ void keep(uint32_t slots) {
+}
+// channels 32 cg .. + 31: two operands
+template <int HD>
+__device__ __forceinline__ void value_ops(std::integral_constant<int, 4>, f16x8 (&op)[2], uint32_t lds, int cg, int lane, uint32_t magic) {
+    constexpr int CODES = Unit<HD, 4>::CODES;
+    const u32x4 w = Unit<HD, 4>::piece(lds + CODES + cg / 2 * 1024 + lane * 16).q;
+    const uint32_t par = lds + 2 * CODES + 4 * HD + cg * 128 + lane / 16 * 32;
+    Half8 u, m, o[2];
+    u.q = Unit<HD, 4>::piece(par).q;
+    m.q = Unit<HD, 4>::piece(par + 16).q;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (!(slots >> e & 1))
-#pragma unroll
-                for (int n = 0; n < HD / 32; ++n) u[n][e] = m[n][e] = 0;
+    for (int i = 0; i < 4; ++i) {
+        o[0].h[i] = __builtin_elementwise_fma(cg % 2 == 0 ? codes2<0>(w[i], magic) : codes2<8>(w[i], magic), u.h[i], m.h[i]);
+        o[1].h[i] = __builtin_elementwise_fma(cg % 2 == 0 ? codes2<4>(w[i], magic) : codes2<12>(w[i], magic), u.h[i], m.h[i]);
     }
-    __device__ __forceinline__ f16x8 operand(int cb) const {
-        const uint4 x = c[cb / 4];
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        const f16x8 un = u[cb / 2], le = m[cb / 2];
-        union {
-            f16x2 h[4];
-            f16x8 v;
-        } o;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f16x2 k;
-            switch (cb % 4) {
-                case 0: k = codes2<0>(w[i]); break;
-                case 1: k = codes2<4>(w[i]); break;
-                case 2: k = codes2<8>(w[i]); break;
-                default: k = codes2<12>(w[i]); break;
-            }
-            o.h[i] = __builtin_elementwise_fma(k, (f16x2){un[2 * i], un[2 * i + 1]}, (f16x2){le[2 * i], le[2 * i + 1]});
-        }
-        return o.v;
-    }
-};
+    op[0] = o[0].v;
+    op[1] = o[1].v;
+}
 
 struct StepScore {
     float sl, kc, capl;     // as in exp_attn.hip: scale log2 e; 2 scale log2 e / cap; cap log2 e
@@ -577,6 +551,9 @@ struct StepScore {
 // 2^-24, which is 2^-31 of the largest, are there.
 constexpr float REF_BELOW = 7.f, REF_MOVE = 15.f;
 constexpr float STEP_NONE = -__builtin_inff();
+// units of a wave's ring
+template <int HD, int BITS>
+constexpr int STEP_DEPTH = BITS == 16 ? 2 : HD == 128 ? 3 : 4;
 
 template <int HD, int BITS, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q, const float* __restrict__ slopes,
@@ -586,7 +563,10 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     using Lay = Layout<HD, BITS>;
     using vec = typename Elem<BITS>::vec;
     constexpr int NK = HD / 32, NV = HD / 16;
-    __shared__ __attribute__((aligned(16))) float sum[4][16][HD + 4];
+    constexpr int DEPTH = STEP_DEPTH<HD, BITS>, BYTES = Unit<HD, BITS>::BYTES, LOADS = Unit<HD, BITS>::LOADS;
+    constexpr bool RAW = !CAP && !BIAS;
+    constexpr int RING = 4 * DEPTH * BYTES, SUMS = 4 * 16 * (HD + 4) * 4;
+    __shared__ uint4 space[(RING > SUMS ? RING : SUMS) / 16];          // the waves' units, then their sums
     __shared__ float2 ml[4][16];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
     // blocks of 16 query heads of a key head side by side: they read the same pages
@@ -654,33 +634,52 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     for (int cb = 0; cb < NV; ++cb) acc[cb] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float ref = STEP_NONE, lsum = 0.f;
 
-    auto unit = [&](auto edge_c, const Keys<HD, BITS>& kk, Values<HD, BITS>& vv, int at, auto&& then) {
-        constexpr bool EDGE = decltype(edge_c)::value;
+    uint32_t magic;
+    asm("v_mov_b32 %0, 0x64006400" : "=v"(magic));
+    const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_address(space) + w * DEPTH * BYTES);
+    const std::integral_constant<int, BITS> bits;
+
+    auto unit = [&](uint32_t at_lds, int at) {
+        const bool edge = at * UNIT < vis.first || at * UNIT + UNIT > vis.len;
+        const int tok0 = at * UNIT + 4 * g;
         f32x4 s[2];
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
             s[blk] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if constexpr (BITS == 16) {
 #pragma unroll
-            for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(kk.operand(blk, ks), qf[ks], s[blk]);
+                for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(key_op<HD>(bits, at_lds, blk, ks, lane, magic), qf[ks], s[blk]);
+            } else {
+                vec kop[NK];
+                key_ops4<HD>(kop, at_lds, blk, lane, magic);
+#pragma unroll
+                for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(kop[ks], qf[ks], s[blk]);
+            }
         }
-        then();         // the keys' registers are free
-        const int tok0 = at * UNIT + 4 * g;
         const float far = BIAS ? (float)(vis.len - 1 - tok0) : 0.f;
         float x[8], top = STEP_NONE;
-        uint32_t slots = 0xffu;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int tok = (e & 3) + 16 * (e >> 2);
-            float y = s[e >> 2][e & 3] * mul;
+            float y = RAW ? s[e >> 2][e & 3] : s[e >> 2][e & 3] * mul;
             if (CAP) y = fmaf(-2.f * sc.capl, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f), sc.capl);
-            if (BIAS) y = fmaf(-slope, far - (float)tok, y);
-            if (EDGE && (tok0 + tok >= vis.len || tok0 + tok < vis.first)) {
-                y = STEP_NONE;
-                slots &= ~(1u << e);
-            }
+            if (BIAS) y = fmaf(-slope, far - (float)((e & 3) + 16 * (e >> 2)), y);
             x[e] = y;
-            top = fmaxf(top, y);
         }
+        if (edge) {
+            uint32_t slots = 0xffu;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int tok = tok0 + (e & 3) + 16 * (e >> 2);
+                if (tok >= vis.len || tok < vis.first) {
+                    x[e] = STEP_NONE;
+                    slots &= ~(1u << e);
+                }
+            }
+            Unit<HD, BITS>::keep(at_lds, slots, lane);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
+        if (RAW) top *= mul;
         if (__any(top > ref + REF_MOVE)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
@@ -697,48 +696,48 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
         vec p;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float y = __builtin_amdgcn_exp2f(x[e] - by);
+            const float y = __builtin_amdgcn_exp2f(RAW ? fmaf(x[e], mul, -by) : x[e] - by);
             lsum += y;          // (unrounded: L is a result)
             if constexpr (BITS == 16) p[e] = (__bf16)y;
             else p[e] = (_Float16)y;
         }
-        if (EDGE) vv.keep(slots);
 #pragma unroll
-        for (int cb = 0; cb < NV; ++cb) acc[cb] = mfma_step(vv.operand(cb), p, acc[cb]);
+        for (int cg = 0; cg < HD / 32; ++cg) {
+            vec op[2];
+            value_ops<HD>(bits, op, at_lds, cg, lane, magic);
+#pragma unroll
+            for (int n = 0; n < 2; ++n) acc[2 * cg + n] = mfma_step(op[n], p, acc[2 * cg + n]);
+        }
     };
 
-    // Page numbers of the wave's next 64 units, one a lane.  Keys and values of the next unit are asked for as soon as their registers are
-    // free, one product ahead.
-    Keys<HD, BITS> kk;
-    Values<HD, BITS> vv;
+    // Page numbers of the wave's next 64 units, one a lane; units of pages that are not there are passed over.  DEPTH units are on the way
+    // or in use at any time.
     const int upp = pg.page / UNIT;
     while (u < u_end) {
         const int mine = u + 4 * lane;
         const int ids = mine < u_end ? page_of(pg, b, mine * UNIT) : -1;
-        const int n = min(64, (u_end - u + 3) / 4);
-        uint64_t have = __ballot(ids >= 0);
-        if (n < 64) have &= (1ULL << n) - 1;
-        auto block_of = [&](int i) {
-            const int id = __builtin_amdgcn_readlane(ids, i);
-            return pool + ((size_t)id * pg.Hk + hk) * Lay::block(pg.page);
+        uint64_t have = __ballot(ids >= 0), ahead = have;
+        auto issue = [&](int slot) {
+            const int i = __builtin_ctzll(ahead);
+            ahead &= ahead - 1;
+            const uint64_t block = uniform64((uint64_t)(pool + ((size_t)__builtin_amdgcn_readlane(ids, i) * pg.Hk + hk) * Lay::block(pg.page)));
+            Unit<HD, BITS>::load(ring + slot * BYTES, block, pg.page, (u + 4 * i) & (upp - 1), lane);
         };
-        if (have != 0) {
-            int i = __builtin_ctzll(have);
-            kk.load(block_of(i), pg, (u + 4 * i) & (upp - 1), lane);
-            vv.load(block_of(i), pg, (u + 4 * i) & (upp - 1), lane);
-            while (have != 0) {
-                have &= have - 1;
-                const int at = u + 4 * i, next = have != 0 ? __builtin_ctzll(have) : i;
-                const char* block = block_of(next);
-                const int in = (u + 4 * next) & (upp - 1);
-                auto then = [&]() {
-                    if (have != 0) kk.load(block, pg, in, lane);
-                };
-                if (at * UNIT < vis.first || at * UNIT + UNIT > vis.len) unit(std::true_type{}, kk, vv, at, then);
-                else unit(std::false_type{}, kk, vv, at, then);
-                if (have != 0) vv.load(block, pg, in, lane);
-                i = next;
+#pragma unroll
+        for (int n = 0; n < DEPTH; ++n)
+            if (ahead != 0) issue(n);
+        int slot = 0;
+        while (have != 0) {
+            const int i = __builtin_ctzll(have);
+            have &= have - 1;
+            if (__popcll(have) >= DEPTH - 1) dma_arrived<(DEPTH - 1) * LOADS>();
+            else dma_arrived<0>();
+            unit(ring + slot * BYTES, u + 4 * i);
+            if (ahead != 0) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the slot's reads are over
+                issue(slot);
             }
+            slot = slot == DEPTH - 1 ? 0 : slot + 1;
         }
         u += 256;
     }
@@ -746,7 +745,9 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     // the four waves' parts
     lsum += __shfl_xor(lsum, 16);
     lsum += __shfl_xor(lsum, 32);
+    float(*sum)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(space);
     if (g == 0) ml[w][r16] = make_float2(ref, lsum);
+    __syncthreads();            // every wave is through with its units
 #pragma unroll
     for (int cb = 0; cb < NV; ++cb) *(f32x4*)&sum[w][r16][16 * cb + 4 * g] = acc[cb];
     __syncthreads();

@@ -107,29 +107,22 @@ struct Tile {
         return (uint32_t)(row / RUN * STEP + row % RUN * 2 * HD + (piece ^ turn(row)) * 16);
     }
 };
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
-}
-// rows row0 .. row0 + 63 of a head of T rows (those past its end as its last one) into a tile; tile_arrived() before the barrier after
-// which they are read.  (Inline, since the compiler would make every LDS read wait for it.)
+// rows row0 .. row0 + 63 of a head of T rows (those past its end as its last one) into a tile; dma_arrived() before the barrier after
+// which they are read
 template <int HD>
 __device__ __forceinline__ void tile_load(const Tile<HD>& t, const bf16_t* __restrict__ head, int row0, int T, int lane, int w) {
     using TL = Tile<HD>;
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(t.at));
-    const uint64_t from = (uint64_t)(head + (size_t)row0 * HD);
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)from), hi = __builtin_amdgcn_readfirstlane((uint32_t)(from >> 32));
-    const uint64_t tile0 = (uint64_t)hi << 32 | lo;
+    const uint64_t tile0 = uniform64((uint64_t)(head + (size_t)row0 * HD));
     const int last = T - 1 - row0, row = lane / TL::PIECES;
     const uint32_t piece = (uint32_t)(lane % TL::PIECES ^ TL::turn(row)) * 16;      // (turn() is the same in every KB)
 #pragma unroll
     for (int q = 0; q < HD / 32; ++q) {
         const int run = 4 * q + w;
         const uint32_t off = (uint32_t)min(run * TL::RUN + row, last) * (2 * HD) + piece;
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(tile0), "s"(base + run * TL::STEP)
-                     : "memory", "m0");
+        dma16(tile0, off, base + run * TL::STEP);
     }
 }
-__device__ __forceinline__ void tile_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // A lane's addresses in a tile
 template <int HD>
@@ -144,7 +137,6 @@ struct Reads {
             col[x] = Tile<HD>::place(4 * h + (r16 >> 2) + (HD == 32 ? 8 * x : 0), (HD == 32 ? 0 : 4 * x) + 2 * odd + (r16 >> 1 & 1)) + 8 * (r16 & 1);
     }
 };
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 // rows 32 blk + r32, features 16 ks + 8 h .. + 7 (A or B operand of a contraction over the features); tile: its address
 template <int HD>
 __device__ __forceinline__ bf16x8 row_op(uint32_t tile, const Reads<HD>& rd, int blk, int ks) {
@@ -352,7 +344,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
         tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
         tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
     }
-    tile_arrived();
+    dma_arrived<0>();
     __syncthreads();
     for (int t = t_lo; t < t_hi; ++t) {
         const int buf = (t - t_lo) & 1, key0 = t * AT;
@@ -365,7 +357,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
             lds_barrier();
         }
         if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
-        tile_arrived();
+        dma_arrived<0>();
         __syncthreads();
     }
 
@@ -557,7 +549,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
         tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
         tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
     }
-    tile_arrived();
+    dma_arrived<0>();
     __syncthreads();
     for (int t = t_lo; t < t_hi; ++t) {
         const int buf = (t - t_lo) & 1, key0 = t * AT;
@@ -570,7 +562,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
             lds_barrier();
         }
         if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
-        tile_arrived();
+        dma_arrived<0>();
         __syncthreads();
     }
 
@@ -763,7 +755,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
         load(t, head0 + gt, 0);
         store(0);
     }
-    tile_arrived();
+    dma_arrived<0>();
     __syncthreads();
     while (t >= 0) {
         const int tn = advance(), gn = g;
@@ -783,7 +775,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
         t = tn;
         gt = gn;
         e = en;
-        tile_arrived();
+        dma_arrived<0>();
         __syncthreads();
     }
 

@@ -95,6 +95,25 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// 16 bytes a lane from memory (base + off) to LDS, lane after lane from address `lds` on, with no register between.  Inline, since the
+// compiler would make every later LDS read wait for it: dma_arrived() (and, for other waves' data, a barrier) before it is read, and
+// reads of what it overwrites have to be over.
+__device__ __forceinline__ void dma16(uint64_t base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+template <int LEFT>     // all but the last LEFT of them (and of any other load)
+__device__ __forceinline__ void dma_arrived() {
+    static_assert(LEFT >= 0 && LEFT < 64, "the counter's range");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+__device__ __forceinline__ uint64_t uniform64(uint64_t x) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
 // Cross-lane sums without the LDS pipe: v_permlane16_swap / v_permlane32_swap exchange 16-lane rows (resp.
 // 32-lane halves) between two registers.
 __device__ __forceinline__ float xor16_sum(float x) {   // x + (value in lane ^ 16), in every lane
