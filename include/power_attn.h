@@ -256,7 +256,8 @@ pa_status power_attn_exp_bwd(const pa_exp_problem* prob, const void* Q, const vo
  * lengths and positions: DEVICE int32 [B].  Nothing of them is read by the host, so a captured graph can be replayed with others
  * in the same place.  A page index outside 0 .. num_pages - 1 stands for no page: nothing is written there, reads give zeros,
  * and a step leaves its tokens out.  Two sequences may share pages that are only read.  d in {64, 128}.  Alignment: pool, K, V, Q, q, o, cos, sin 16 bytes, the other
- * arrays that of their type.  Up to 65535 sequences and heads, 2^30 positions a sequence and 2^29 rows a call. */
+ * arrays that of their type.  Up to 65535 sequences and heads, 2^30 positions a sequence, less than 2^36 in all,
+ * and 2^29 rows a call. */
 typedef struct {
     int   B, H, Hk, d;              /* sequences, query heads, key heads (H a multiple of Hk), head size */
     int   page;                     /* tokens per page: a power of two, 32 .. 1024 */

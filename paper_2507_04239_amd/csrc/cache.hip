@@ -375,13 +375,14 @@ __global__ __launch_bounds__(256) void k_cache_read(const char* __restrict__ poo
 }
 
 // ---- one token's attention -----------------------------------------------------------------------------------------
-// Work is cut on the device, since lengths are known there only: the visible units of all sequences together are dealt in chunks of
-// one size, so that long sequences get more workgroups than short ones and a captured launch follows the lengths of its replay.
-// A sequence of one chunk is finished by its workgroup; the parts of the others are joined by a second kernel.
-constexpr int CHUNK_MIN = 4;            // units: one for each wave
+// Work is cut on the device, since lengths are known there only, so that a captured launch follows the lengths of its replay: the visible
+// units of all sequences, one behind the other, are dealt to the workgroups of a key head in runs of one length, as many as the chip
+// holds at once.  A run may end inside a sequence and begin another: each piece of a sequence leaves its sums in a slot of its own
+// (workgroup + sequence, which no two pieces share) and a second kernel joins them; a sequence that lies in one run is finished there.
+constexpr int RUN_MIN = 4;              // units: one for each wave
 struct Split {
-    int target;             // chunks that the units are dealt to (a sequence's last chunk may be shorter: up to B more)
-    int slots;              // target + B
+    int runs;               // workgroups per key head (and block of query heads)
+    int slots;              // runs + B
 };
 struct Visible {
     int len, first;         // tokens held, first token seen
@@ -410,16 +411,13 @@ __device__ __forceinline__ int wave_scan(int x, int lane) {     // inclusive
     }
     return x;
 }
-__device__ __forceinline__ int chunk_units(const int* lens, int B, const Pages& pg, int window, int target, int lane) {
-    // (64-bit: lengths up to 2^30 of many sequences)
-    unsigned long long total = 0;
-    for (int base = 0; base < B; base += 64) {
-        const int u = visible(lens, base + lane, B, pg, window).units;
-        total += (unsigned)wave_sum(u & 0xffff) + ((unsigned long long)(unsigned)wave_sum(u >> 16) << 16);
-    }
-    const unsigned long long c = (total + target - 1) / target;
-    return max(CHUNK_MIN, (int)min(c, 1ULL << 26));     // (a sequence has at most 2^25 units)
+// (the units of all sequences together number less than 2^31)
+__device__ __forceinline__ int total_units(const int* lens, int B, const Pages& pg, int window, int lane) {
+    int total = 0;
+    for (int base = 0; base < B; base += 64) total += wave_sum(visible(lens, base + lane, B, pg, window).units);
+    return total;
 }
+__device__ __forceinline__ int run_units(int total, int runs) { return max(RUN_MIN, total / runs + (total % runs != 0 ? 1 : 0)); }
 
 template <int BITS>
 struct Elem {
@@ -571,224 +569,227 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
     // blocks of 16 query heads of a key head side by side: they read the same pages
     const int mblks = (G + 15) / 16, per = pg.Hk * mblks;
-    const int slot = (int)(blockIdx.x / (unsigned)per), rest = (int)(blockIdx.x - (unsigned)slot * (unsigned)per);
+    const int run = (int)(blockIdx.x / (unsigned)per), rest = (int)(blockIdx.x - (unsigned)run * (unsigned)per);
     const int hk = rest / mblks, mb = rest - hk * mblks;
-
-    // the slot's sequence and place in it
-    const int C = chunk_units(lens, B, pg, window, split.target, lane);
-    int b = -1, nth = 0, chunks = 0, before = 0;
-    Visible vis{0, 0, 0, 0};
-    for (int base = 0; base < B && b < 0; base += 64) {
-        const Visible v = visible(lens, base + lane, B, pg, window);
-        const int n = (v.units + C - 1) / C, upto = before + wave_scan(n, lane);
-        const uint64_t past = __ballot(upto > slot);
-        if (past != 0) {
-            const int at = __builtin_ctzll(past);
-            b = base + at;
-            chunks = __builtin_amdgcn_readlane(n, at);
-            nth = slot - (__builtin_amdgcn_readlane(upto, at) - chunks);
-            vis = {__builtin_amdgcn_readlane(v.len, at), __builtin_amdgcn_readlane(v.first, at), __builtin_amdgcn_readlane(v.unit0, at),
-                   __builtin_amdgcn_readlane(v.units, at)};
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
-    }
-    if (b < 0) return;
-    const int u_end = vis.unit0 + min(vis.units, (nth + 1) * C);       // (nth + 1) C <= units + C, and both are below 2^26
-    int u = vis.unit0 + nth * C + w;
-
-    // the head of this lane's column
-    const int hq = 16 * mb + r16, head = hk * G + min(hq, G - 1);
-    vec qf[NK];
-    float factor = 1.f;
-    {
-        Frag raw[NK];
-        float top = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < NK; ++ks) {
-            raw[ks].u = *(const uint4*)(q + ((size_t)b * H + head) * HD + 32 * ks + 8 * g);
-            if (hq >= G) raw[ks].u = make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)raw[ks].v[e]));
-        }
-        if constexpr (BITS == 16) {
-#pragma unroll
-            for (int ks = 0; ks < NK; ++ks) qf[ks] = raw[ks].v;
-        } else {
-            // q over a power of two, so that bf16's range fits fp16's; the scores take it back
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const int ex = top > 0.f && top < __builtin_inff() ? ilogbf(top) : 0;
-            factor = ldexpf(1.f, ex);
-            const float inv = ldexpf(1.f, -ex);
-#pragma unroll
-            for (int ks = 0; ks < NK; ++ks)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) qf[ks][e] = (_Float16)((float)raw[ks].v[e] * inv);
-        }
-    }
-    const float slope = BIAS ? slopes[head] * 1.44269504088896340736f : 0.f;
-    const float mul = (CAP ? sc.kc : sc.sl) * factor;
-
-    f32x4 acc[NV];
-#pragma unroll
-    for (int cb = 0; cb < NV; ++cb) acc[cb] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    float ref = STEP_NONE, lsum = 0.f;
+    const int total = total_units(lens, B, pg, window, lane), C = run_units(total, split.runs);
+    if (run > (total - 1) / C || total == 0) return;
+    const int begin = run * C, end = begin + min(C, total - begin);
 
     uint32_t magic;
     asm("v_mov_b32 %0, 0x64006400" : "=v"(magic));
     const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_address(space) + w * DEPTH * BYTES);
     const std::integral_constant<int, BITS> bits;
+    const int upp = pg.page / UNIT;
 
-    auto unit = [&](uint32_t at_lds, int at) {
-        const bool edge = at * UNIT < vis.first || at * UNIT + UNIT > vis.len;
-        const int tok0 = at * UNIT + 4 * g;
-        f32x4 s[2];
+    // units `u` to `u_end` of sequence b, which is cut in several pieces or whole
+    auto piece = [&](int b, Visible vis, int u, int u_end, bool whole) {
+        // the head of this lane's column
+        const int hq = 16 * mb + r16, head = hk * G + min(hq, G - 1);
+        vec qf[NK];
+        float factor = 1.f;
+        {
+            Frag raw[NK];
+            float top = 0.f;
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            s[blk] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            for (int ks = 0; ks < NK; ++ks) {
+                raw[ks].u = *(const uint4*)(q + ((size_t)b * H + head) * HD + 32 * ks + 8 * g);
+                if (hq >= G) raw[ks].u = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)raw[ks].v[e]));
+            }
             if constexpr (BITS == 16) {
 #pragma unroll
-                for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(key_op<HD>(bits, at_lds, blk, ks, lane, magic), qf[ks], s[blk]);
+                for (int ks = 0; ks < NK; ++ks) qf[ks] = raw[ks].v;
             } else {
-                vec kop[NK];
-                key_ops4<HD>(kop, at_lds, blk, lane, magic);
+                // q over a power of two, so that bf16's range fits fp16's; the scores take it back
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const int ex = top > 0.f && top < __builtin_inff() ? ilogbf(top) : 0;
+                factor = ldexpf(1.f, ex);
+                const float inv = ldexpf(1.f, -ex);
 #pragma unroll
-                for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(kop[ks], qf[ks], s[blk]);
+                for (int ks = 0; ks < NK; ++ks)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) qf[ks][e] = (_Float16)((float)raw[ks].v[e] * inv);
             }
         }
-        const float far = BIAS ? (float)(vis.len - 1 - tok0) : 0.f;
-        float x[8], top = STEP_NONE;
+        const float slope = BIAS ? slopes[head] * 1.44269504088896340736f : 0.f;
+        const float mul = (CAP ? sc.kc : sc.sl) * factor;
+
+        f32x4 acc[NV];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float y = RAW ? s[e >> 2][e & 3] : s[e >> 2][e & 3] * mul;
-            if (CAP) y = fmaf(-2.f * sc.capl, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f), sc.capl);
-            if (BIAS) y = fmaf(-slope, far - (float)((e & 3) + 16 * (e >> 2)), y);
-            x[e] = y;
-        }
-        if (edge) {
-            uint32_t slots = 0xffu;
+        for (int cb = 0; cb < NV; ++cb) acc[cb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        float ref = STEP_NONE, lsum = 0.f;
+
+        auto unit = [&](uint32_t at_lds, int at) {
+            const bool edge = at * UNIT < vis.first || at * UNIT + UNIT > vis.len;
+            const int tok0 = at * UNIT + 4 * g;
+            f32x4 s[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int tok = tok0 + (e & 3) + 16 * (e >> 2);
-                if (tok >= vis.len || tok < vis.first) {
-                    x[e] = STEP_NONE;
-                    slots &= ~(1u << e);
+            for (int blk = 0; blk < 2; ++blk) {
+                s[blk] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                if constexpr (BITS == 16) {
+#pragma unroll
+                    for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(key_op<HD>(bits, at_lds, blk, ks, lane, magic), qf[ks], s[blk]);
+                } else {
+                    vec kop[NK];
+                    key_ops4<HD>(kop, at_lds, blk, lane, magic);
+#pragma unroll
+                    for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(kop[ks], qf[ks], s[blk]);
                 }
             }
-            Unit<HD, BITS>::keep(at_lds, slots, lane);
+            const float far = BIAS ? (float)(vis.len - 1 - tok0) : 0.f;
+            float x[8], top = STEP_NONE;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float y = RAW ? s[e >> 2][e & 3] : s[e >> 2][e & 3] * mul;
+                if (CAP) y = fmaf(-2.f * sc.capl, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.f), sc.capl);
+                if (BIAS) y = fmaf(-slope, far - (float)((e & 3) + 16 * (e >> 2)), y);
+                x[e] = y;
+            }
+            if (edge) {
+                uint32_t slots = 0xffu;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int tok = tok0 + (e & 3) + 16 * (e >> 2);
+                    if (tok >= vis.len || tok < vis.first) {
+                        x[e] = STEP_NONE;
+                        slots &= ~(1u << e);
+                    }
+                }
+                Unit<HD, BITS>::keep(at_lds, slots, lane);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
+            if (RAW) top *= mul;
+            if (__any(top > ref + REF_MOVE)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float to = fmaxf(ref, top - REF_BELOW);
+                const float f = to == STEP_NONE ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+                ref = to;
+                lsum *= f;
+#pragma unroll
+                for (int cb = 0; cb < NV; ++cb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[cb][r] *= f;
+            }
+            const float by = ref == STEP_NONE ? 0.f : ref;
+            vec p;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = __builtin_amdgcn_exp2f(RAW ? fmaf(x[e], mul, -by) : x[e] - by);
+                lsum += y;          // (unrounded: L is a result)
+                if constexpr (BITS == 16) p[e] = (__bf16)y;
+                else p[e] = (_Float16)y;
+            }
+#pragma unroll
+            for (int cg = 0; cg < HD / 32; ++cg) {
+                vec op[2];
+                value_ops<HD>(bits, op, at_lds, cg, lane, magic);
+#pragma unroll
+                for (int n = 0; n < 2; ++n) acc[2 * cg + n] = mfma_step(op[n], p, acc[2 * cg + n]);
+            }
+        };
+
+        // Page numbers of the wave's next 64 units, one a lane; units of pages that are not there are passed over.  DEPTH units are on the way
+        // or in use at any time.
+        u += w;
+        while (u < u_end) {
+            const int mine = u + 4 * lane;
+            const int ids = mine < u_end ? page_of(pg, b, mine * UNIT) : -1;
+            uint64_t have = __ballot(ids >= 0), ahead = have;
+            auto issue = [&](int slot) {
+                const int i = __builtin_ctzll(ahead);
+                ahead &= ahead - 1;
+                const uint64_t block = uniform64((uint64_t)(pool + ((size_t)__builtin_amdgcn_readlane(ids, i) * pg.Hk + hk) * Lay::block(pg.page)));
+                Unit<HD, BITS>::load(ring + slot * BYTES, block, pg.page, (u + 4 * i) & (upp - 1), lane);
+            };
+#pragma unroll
+            for (int n = 0; n < DEPTH; ++n)
+                if (ahead != 0) issue(n);
+            int slot = 0;
+            while (have != 0) {
+                const int i = __builtin_ctzll(have);
+                have &= have - 1;
+                if (__popcll(have) >= DEPTH - 1) dma_arrived<(DEPTH - 1) * LOADS>();
+                else dma_arrived<0>();
+                unit(ring + slot * BYTES, u + 4 * i);
+                if (ahead != 0) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the slot's reads are over
+                    issue(slot);
+                }
+                slot = slot == DEPTH - 1 ? 0 : slot + 1;
+            }
+            u += 256;
         }
+
+        // the four waves' parts
+        lsum += __shfl_xor(lsum, 16);
+        lsum += __shfl_xor(lsum, 32);
+        float(*sum)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(space);
+        if (g == 0) ml[w][r16] = make_float2(ref, lsum);
+        __syncthreads();            // every wave is through with its units
 #pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
-        if (RAW) top *= mul;
-        if (__any(top > ref + REF_MOVE)) {
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float to = fmaxf(ref, top - REF_BELOW);
-            const float f = to == STEP_NONE ? 1.f : __builtin_amdgcn_exp2f(ref - to);
-            ref = to;
-            lsum *= f;
+        for (int cb = 0; cb < NV; ++cb) *(f32x4*)&sum[w][r16][16 * cb + 4 * g] = acc[cb];
+        __syncthreads();
+        constexpr int LPH = 16;             // lanes per head
+        const int h = tid / LPH, c0 = tid % LPH;
+        float top = STEP_NONE, z = 0.f, f[4];
 #pragma unroll
-            for (int cb = 0; cb < NV; ++cb)
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i][h].x);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[cb][r] *= f;
+        for (int i = 0; i < 4; ++i) {
+            f[i] = ml[i][h].x == STEP_NONE ? (ml[i][h].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[i][h].x - top);
+            z += f[i] * ml[i][h].y;
         }
-        const float by = ref == STEP_NONE ? 0.f : ref;
-        vec p;
+        const int hd = hk * G + 16 * mb + h;
+        const float inv = whole ? (z != 0.f ? 1.f / z : 0.f) : 1.f;
+        const size_t slot = (size_t)run + b;
+        if (16 * mb + h < G) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float y = __builtin_amdgcn_exp2f(RAW ? fmaf(x[e], mul, -by) : x[e] - by);
-            lsum += y;          // (unrounded: L is a result)
-            if constexpr (BITS == 16) p[e] = (__bf16)y;
-            else p[e] = (_Float16)y;
-        }
+            for (int c = 4 * c0; c < HD; c += 4 * LPH) {
+                f32x4 x = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int cg = 0; cg < HD / 32; ++cg) {
-            vec op[2];
-            value_ops<HD>(bits, op, at_lds, cg, lane, magic);
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 y = *(const f32x4*)&sum[i][h][c];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) acc[2 * cg + n] = mfma_step(op[n], p, acc[2 * cg + n]);
+                    for (int r = 0; r < 4; ++r) x[r] += f[i] * y[r];
+                }
+                if (whole) {
+                    bf16x4 y;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) y[r] = (__bf16)(x[r] * inv);
+                    *(bf16x4*)(o + ((size_t)b * H + hd) * HD + c) = y;
+                } else {
+                    *(f32x4*)(part + (slot * H + hd) * HD + c) = x;
+                }
+            }
+            if (c0 == 0) {
+                if (!whole) stat[slot * H + hd] = make_float2(top, z);
+                else if (L != nullptr) L[(size_t)b * H + hd] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.69314718055994530942f : STEP_NONE;
+            }
         }
     };
 
-    // Page numbers of the wave's next 64 units, one a lane; units of pages that are not there are passed over.  DEPTH units are on the way
-    // or in use at any time.
-    const int upp = pg.page / UNIT;
-    while (u < u_end) {
-        const int mine = u + 4 * lane;
-        const int ids = mine < u_end ? page_of(pg, b, mine * UNIT) : -1;
-        uint64_t have = __ballot(ids >= 0), ahead = have;
-        auto issue = [&](int slot) {
-            const int i = __builtin_ctzll(ahead);
-            ahead &= ahead - 1;
-            const uint64_t block = uniform64((uint64_t)(pool + ((size_t)__builtin_amdgcn_readlane(ids, i) * pg.Hk + hk) * Lay::block(pg.page)));
-            Unit<HD, BITS>::load(ring + slot * BYTES, block, pg.page, (u + 4 * i) & (upp - 1), lane);
-        };
-#pragma unroll
-        for (int n = 0; n < DEPTH; ++n)
-            if (ahead != 0) issue(n);
-        int slot = 0;
-        while (have != 0) {
-            const int i = __builtin_ctzll(have);
-            have &= have - 1;
-            if (__popcll(have) >= DEPTH - 1) dma_arrived<(DEPTH - 1) * LOADS>();
-            else dma_arrived<0>();
-            unit(ring + slot * BYTES, u + 4 * i);
-            if (ahead != 0) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the slot's reads are over
-                issue(slot);
-            }
-            slot = slot == DEPTH - 1 ? 0 : slot + 1;
+    int before = 0;
+    for (int base = 0; base < B && before < end; base += 64) {
+        const Visible v = visible(lens, base + lane, B, pg, window);
+        const int upto = before + wave_scan(v.units, lane);
+        uint64_t mine = __ballot(v.units > 0 && upto > begin && upto - v.units < end);
+        for (; mine != 0; mine &= mine - 1) {
+            const int at = __builtin_ctzll(mine);
+            const Visible vis{__builtin_amdgcn_readlane(v.len, at), __builtin_amdgcn_readlane(v.first, at), __builtin_amdgcn_readlane(v.unit0, at),
+                              __builtin_amdgcn_readlane(v.units, at)};
+            const int last = __builtin_amdgcn_readlane(upto, at), first = last - vis.units;
+            piece(base + at, vis, vis.unit0 + max(begin - first, 0), vis.unit0 + min(end, last) - first, first >= begin && last <= end);
+            __syncthreads();        // the sums have been read: the ring is free
         }
-        u += 256;
-    }
-
-    // the four waves' parts
-    lsum += __shfl_xor(lsum, 16);
-    lsum += __shfl_xor(lsum, 32);
-    float(*sum)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(space);
-    if (g == 0) ml[w][r16] = make_float2(ref, lsum);
-    __syncthreads();            // every wave is through with its units
-#pragma unroll
-    for (int cb = 0; cb < NV; ++cb) *(f32x4*)&sum[w][r16][16 * cb + 4 * g] = acc[cb];
-    __syncthreads();
-    constexpr int LPH = 16;             // lanes per head
-    const int h = tid / LPH, c0 = tid % LPH;
-    if (16 * mb + h >= G) return;
-    float top = STEP_NONE, z = 0.f, f[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, ml[i][h].x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[i] = ml[i][h].x == STEP_NONE ? (ml[i][h].y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml[i][h].x - top);
-        z += f[i] * ml[i][h].y;
-    }
-    const int hd = hk * G + 16 * mb + h;
-    const float inv = chunks == 1 ? (z != 0.f ? 1.f / z : 0.f) : 1.f;
-#pragma unroll
-    for (int c = 4 * c0; c < HD; c += 4 * LPH) {
-        f32x4 x = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 y = *(const f32x4*)&sum[i][h][c];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] += f[i] * y[r];
-        }
-        if (chunks == 1) {
-            bf16x4 y;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = (__bf16)(x[r] * inv);
-            *(bf16x4*)(o + ((size_t)b * H + hd) * HD + c) = y;
-        } else {
-            *(f32x4*)(part + ((size_t)slot * H + hd) * HD + c) = x;
-        }
-    }
-    if (c0 == 0) {
-        if (chunks > 1) stat[(size_t)slot * H + hd] = make_float2(top, z);
-        else if (L != nullptr) L[(size_t)b * H + hd] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * 0.69314718055994530942f : STEP_NONE;
+        before = __builtin_amdgcn_readlane(upto, 63);
     }
 }
 
-// sequences of several chunks; those of none get what an empty row has.  A wave per query head.
+// Sequences in several pieces; those without a unit get what an empty row has.  A wave per query head.
 template <int HD>
 __global__ __launch_bounds__(256) void k_cache_join(const int* __restrict__ lens, const float* __restrict__ part,
                                                     const float2* __restrict__ stat, bf16_t* __restrict__ o, float* __restrict__ L, int B,
@@ -798,14 +799,16 @@ __global__ __launch_bounds__(256) void k_cache_join(const int* __restrict__ lens
     const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= (long long)B * H) return;
     const int b = __builtin_amdgcn_readfirstlane((int)(row / H)), h = __builtin_amdgcn_readfirstlane((int)(row % H));
-    const int C = chunk_units(lens, B, pg, window, split.target, lane);
-    int first = 0, chunks = 0;
+    const int total = total_units(lens, B, pg, window, lane), C = run_units(total, split.runs);
+    int start = 0, units = 0;
     for (int base = 0; base <= b; base += 64) {
-        const int n = (visible(lens, base + lane, B, pg, window).units + C - 1) / C;
-        first += wave_sum(base + lane < b ? n : 0);
-        if (b - base < 64) chunks = __builtin_amdgcn_readlane(n, b - base);
+        const int n = visible(lens, base + lane, B, pg, window).units;
+        start += wave_sum(base + lane < b ? n : 0);
+        if (b - base < 64) units = __builtin_amdgcn_readlane(n, b - base);
     }
+    const int chunks = units > 0 ? (start + units - 1) / C - start / C + 1 : 0;
     if (chunks == 1) return;
+    const size_t first = (size_t)(start / C) + b;
     float top = STEP_NONE;
     for (int i = lane; i < chunks; i += 64) top = fmaxf(top, stat[(size_t)(first + i) * H + h].x);
 #pragma unroll
@@ -834,10 +837,13 @@ Pages pages_of(const pa_cache& c, const int* table) {
     while ((1 << shift) < c.page) ++shift;
     return {table, c.page, shift, c.max_pages, c.num_pages, c.Hk};
 }
+// As many workgroups as are resident together (by their LDS: 1 to 3 a CU), so that all of them have the same work and start once; where
+// a key head would get few, several rounds of them.
 Split split_of(const pa_cache& c) {
     const int per = c.Hk * ((c.H / c.Hk + 15) / 16);
-    const int target = std::max(1, 1024 / per);
-    return {target, target + c.B};
+    const int resident = c.d == 128 ? (c.bits == 4 ? 2 : 1) : (c.bits == 4 ? 3 : 2);
+    const int runs = std::max(8, 256 * resident / per);
+    return {runs, runs + c.B};
 }
 size_t part_bytes(const pa_cache& c) { return align_up((size_t)split_of(c).slots * c.H * c.d * sizeof(float), 256); }
 
@@ -897,7 +903,7 @@ pa_status cache_step(const pa_cache& c, const bf16_t* q, const float* slopes, co
         sc.kc = (float)(2.0 * c.scale / c.cap * 1.44269504088896340736);
         sc.capl = c.cap * 1.44269504088896340736f;
     }
-    const unsigned grid = (unsigned)split.slots * (unsigned)(c.Hk * ((G + 15) / 16));
+    const unsigned grid = (unsigned)split.runs * (unsigned)(c.Hk * ((G + 15) / 16));
     auto launch = [&](auto hd, auto bits, auto cap, auto bias) {
         LaunchScope ls("cache_step", s);
         hipLaunchKernelGGL((k_cache_step<decltype(hd)::value, decltype(bits)::value, decltype(cap)::value, decltype(bias)::value>), dim3(grid),
