@@ -192,13 +192,14 @@ __device__ __forceinline__ bool row_nonfinite(const bf16_t* __restrict__ row, in
 struct Order {
     int H, Hk, G, BHk;      // query heads, key heads, query heads per key head, key heads of the batch
     int group, nblk;        // key heads of a group; blocks of rows of a head
+    int parts;              // workgroups that share the walk of a block of keys
 };
 struct Place {
-    int kv, g, rank;
+    int kv, g, rank;        // g: the query head of the key head's, or the part
 };
 template <bool PER_KEY_HEAD>
 __device__ __forceinline__ bool place(const Order& o, Place& p) {
-    const unsigned per = (unsigned)o.group * (PER_KEY_HEAD ? 1u : (unsigned)o.G);
+    const unsigned per = (unsigned)o.group * (unsigned)(PER_KEY_HEAD ? o.parts : o.G);
     const unsigned row = blockIdx.x / per, x = blockIdx.x - row * per;
     const unsigned z = row / (unsigned)o.nblk;
     p.rank = (int)(row - z * (unsigned)o.nblk);
@@ -594,7 +595,8 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
 // ---- backward: dK, dV -----------------------------------------------------------------------------------------
 // dk[fb][kb] = dK^T / scale: features 32 fb + .., key 32 kb + r32 of the wave's OWN keys; dv likewise.  The walk goes over the
 // query rows of every head that reads the key head; tiles of rows that see none of the block's keys are found 64 at a time from the
-// ends that the preparation left.
+// ends that the preparation left.  Where there are few blocks, each is walked by several workgroups, which take turns at its tiles;
+// their float32 sums (in the order of the registers) are added by k_exp_dkdv_join.
 template <int HD>
 struct BwdShared {
     Tile<HD> q[2], g[2];
@@ -606,7 +608,8 @@ template <int HD, int OWN, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
                                                        const bf16_t* __restrict__ V, const float* __restrict__ slopes,
                                                        const bf16_t* __restrict__ dO, BwdScratch from, bf16_t* __restrict__ dK,
-                                                       bf16_t* __restrict__ dV, Order order, Rows rows, Score sc, float scale) {
+                                                       bf16_t* __restrict__ dV, float4* __restrict__ sums, Order order, Rows rows,
+                                                       Score sc, float scale) {
     constexpr int NJ = OWN / 32, NK = HD / 16, NF = HD / 32, WG = 4 * OWN;
     __shared__ BwdShared<HD> sm;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, h = lane >> 5;
@@ -704,24 +707,28 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
     };
 
     // the tiles of rows that see a key of the block, for one head after the other, 64 tiles at a time
-    int base = -64, g = order.G;
+    int base = -64, g = order.G, turn = 0;
     uint64_t seen = 0, left = 0;
     auto advance = [&]() -> int {
-        while (left == 0) {
-            if (++g < order.G) {
-                left = seen;
-            } else {
-                base += 64;
-                if (base >= ntile) return -1;
-                const int t = base + lane;
-                const int4 e = ends[min(t, ntile - 1)];
-                seen = left = __ballot(t < ntile && !Ends{e.x, e.y, e.z, e.w}.none(j0, WG));
-                g = seen != 0 ? 0 : order.G;
+        for (;;) {
+            while (left == 0) {
+                if (++g < order.G) {
+                    left = seen;
+                } else {
+                    base += 64;
+                    if (base >= ntile) return -1;
+                    const int t = base + lane;
+                    const int4 e = ends[min(t, ntile - 1)];
+                    seen = left = __ballot(t < ntile && !Ends{e.x, e.y, e.z, e.w}.none(j0, WG));
+                    g = seen != 0 ? 0 : order.G;
+                }
             }
+            const int t = base + __builtin_ctzll(left);
+            left &= left - 1;
+            const bool mine = turn == at.g;
+            turn = turn + 1 == order.parts ? 0 : turn + 1;
+            if (mine) return t;
         }
-        const int t = base + __builtin_ctzll(left);
-        left &= left - 1;
-        return t;
     };
     float2 str = make_float2(0.f, 0.f);
     int2 rgr = make_int2(0, 0);
@@ -803,6 +810,18 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
             }
         }
     }
+    if (order.parts > 1) {
+        static_assert(NJ == 1, "a wave's 32 keys");
+        float4* to = sums + ((((size_t)at.g * order.BHk + at.kv) * order.nblk + at.rank) * 4 + w) * (8 * NF * 64) + lane;
+#pragma unroll
+        for (int fb = 0; fb < NF; ++fb)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                to[(4 * fb + k) * 64] = make_float4(dk[fb][0][4 * k], dk[fb][0][4 * k + 1], dk[fb][0][4 * k + 2], dk[fb][0][4 * k + 3]);
+                to[(4 * (NF + fb) + k) * 64] = make_float4(dv[fb][0][4 * k], dv[fb][0][4 * k + 1], dv[fb][0][4 * k + 2], dv[fb][0][4 * k + 3]);
+            }
+        return;
+    }
 #pragma unroll
     for (int kb = 0; kb < NJ; ++kb) {
         const int key = k0 + 32 * kb + r32;
@@ -815,10 +834,37 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
     }
 }
 
+// 32 features of a block's dK (blockIdx.y < HD / 32) or dV from its parts' sums
+template <int HD>
+__global__ __launch_bounds__(256) void k_exp_dkdv_join(const float4* __restrict__ sums, bf16_t* __restrict__ dK, bf16_t* __restrict__ dV,
+                                                       int blocks, int nblk, int parts, int Tk, float scale) {
+    constexpr int NF = HD / 32;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, y = (int)blockIdx.y;
+    const int kv = (int)(blockIdx.x / (unsigned)nblk), key = (int)(blockIdx.x - (unsigned)kv * (unsigned)nblk) * 128 + 32 * w + (lane & 31);
+    if (key >= Tk) return;
+    const size_t part = (size_t)blocks * 4 * (8 * NF * 64);
+    const float4* from = sums + ((size_t)blockIdx.x * 4 + w) * (8 * NF * 64) + y * 4 * 64 + lane;
+    float4 x[4] = {};
+#pragma unroll 2
+    for (int p = 0; p < parts; ++p)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float4 v = from[p * part + k * 64];
+            x[k].x += v.x; x[k].y += v.y; x[k].z += v.z; x[k].w += v.w;
+        }
+    const float f = y >= NF ? 1.f : scale;
+    bf16_t* to = (y >= NF ? dV : dK) + ((size_t)kv * Tk + key) * HD + 32 * (y % NF) + 4 * (lane >> 5);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bf16x4 o = {(__bf16)(x[k].x * f), (__bf16)(x[k].y * f), (__bf16)(x[k].z * f), (__bf16)(x[k].w * f)};
+        *(bf16x4*)(to + 8 * k) = o;
+    }
+}
+
 // ---- launches -----------------------------------------------------------------------------------------------
 // Key heads whose K and V fit half of the memory-side cache go together (attention form: 184 ms a step with all heads, 156 so).
 Order order_of(const pa_exp_problem& pr, int rows_per_block, int len) {
-    Order o{pr.H, pr.Hk, pr.H / pr.Hk, pr.B * pr.Hk, pr.B * pr.Hk, (len + rows_per_block - 1) / rows_per_block};
+    Order o{pr.H, pr.Hk, pr.H / pr.Hk, pr.B * pr.Hk, pr.B * pr.Hk, (len + rows_per_block - 1) / rows_per_block, 1};
     const long long fit = std::max(8LL, (128LL << 20) / (4LL * std::max(pr.T, pr.Tk) * pr.d));
     if (o.BHk > fit) {
         int g = 8;
@@ -828,7 +874,7 @@ Order order_of(const pa_exp_problem& pr, int rows_per_block, int len) {
     return o;
 }
 long long blocks_of(const Order& o, bool per_key_head) {
-    return (long long)((o.BHk + o.group - 1) / o.group) * o.group * (per_key_head ? 1 : o.G) * o.nblk;
+    return (long long)((o.BHk + o.group - 1) / o.group) * o.group * (per_key_head ? o.parts : o.G) * o.nblk;
 }
 
 template <int HD>
@@ -846,6 +892,19 @@ pa_status fwd_t(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, cons
                        mk.slopes, O, L, o, rows, score_of(pr));
     return launch_ok() ? PA_OK : PA_ERR_HIP;
 }
+// Workgroups per block of 128 keys: until there are four per CU, as long as each has 16 tiles or more.  (us, dK/dV and join, one and
+// two or three parts: B2 H12/4 T4095 d64, 256 blocks, 227 and 78 + 15; B2 H16/4 T8192 d128 of documents, 512 blocks, 772 and 512 + 38,
+// four parts 489 + 61.  From 1024 blocks on a part more only adds its sums: B1 H16/8 T16384 d128 2.41 ms and 2.41 + 0.07.)
+int dkdv_parts(const pa_exp_problem& pr) {
+    const Order o = order_of(pr, 128, pr.Tk);
+    const long long jobs = (long long)o.BHk * o.nblk, items = (long long)o.G * ((pr.T + AT - 1) / AT);
+    return (int)std::max(1LL, std::min({(1024 + jobs - 1) / jobs, items / 16, 8LL}));
+}
+size_t part_bytes(const pa_exp_problem& pr) {
+    const int parts = dkdv_parts(pr);
+    const Order o = order_of(pr, 128, pr.Tk);
+    return parts > 1 ? (size_t)parts * o.BHk * o.nblk * 128 * 2 * pr.d * sizeof(float) : 0;
+}
 BwdScratch bwd_scratch(const pa_exp_problem& pr, char* ws) {
     const size_t BHT = (size_t)pr.B * pr.H * pr.T, BT = (size_t)pr.B * pr.T;
     char* range = ws + align_up(BHT * sizeof(float2), 256);
@@ -862,11 +921,19 @@ pa_status bwd_t(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, cons
                            ntile);
         if (!launch_ok()) return PA_ERR_HIP;
     }
+    Order ok = order_of(pr, 128, pr.Tk);
+    ok.parts = dkdv_parts(pr);
+    float4* sums = (float4*)((char*)sc.ends + align_up((size_t)pr.B * ntile * sizeof(int4), 256));
     {
-        const Order o = order_of(pr, 128, pr.Tk);
         LaunchScope ls("exp_bwd_dkdv", s);
-        hipLaunchKernelGGL((k_exp_dkdv<HD, 32, Shape<HD>::DKDV_WPE, CAP, BIAS>), dim3((unsigned)blocks_of(o, true)), dim3(256), 0, s, Q, K,
-                           V, mk.slopes, dO, sc, dK, dV, o, rows, score_of(pr), pr.scale);
+        hipLaunchKernelGGL((k_exp_dkdv<HD, 32, Shape<HD>::DKDV_WPE, CAP, BIAS>), dim3((unsigned)blocks_of(ok, true)), dim3(256), 0, s, Q, K,
+                           V, mk.slopes, dO, sc, dK, dV, sums, ok, rows, score_of(pr), pr.scale);
+        if (!launch_ok()) return PA_ERR_HIP;
+    }
+    if (ok.parts > 1) {
+        LaunchScope ls("exp_bwd_join", s);
+        hipLaunchKernelGGL((k_exp_dkdv_join<HD>), dim3((unsigned)(ok.BHk * ok.nblk), HD / 16), dim3(256), 0, s, sums, dK, dV, ok.BHk * ok.nblk,
+                           ok.nblk, ok.parts, pr.Tk, pr.scale);
         if (!launch_ok()) return PA_ERR_HIP;
     }
     const Order o = order_of(pr, 128, pr.T);
@@ -909,7 +976,7 @@ bool exp_grid_ok(const pa_exp_problem& pr) {
 size_t exp_workspace_bytes(const pa_exp_problem& pr, bool backward) {
     if (!backward) return 0;
     const BwdScratch sc = bwd_scratch(pr, nullptr);
-    return (size_t)(char*)sc.ends + align_up((size_t)pr.B * ((pr.T + AT - 1) / AT) * sizeof(int4), 256);
+    return (size_t)(char*)sc.ends + align_up((size_t)pr.B * ((pr.T + AT - 1) / AT) * sizeof(int4), 256) + part_bytes(pr);
 }
 
 pa_status exp_fwd(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, const bf16_t* V, ExpMask mk, bf16_t* O, float* L, char*,
