@@ -192,18 +192,19 @@ __device__ __forceinline__ bool row_nonfinite(const bf16_t* __restrict__ row, in
 struct Order {
     int H, Hk, G, BHk;      // query heads, key heads, query heads per key head, key heads of the batch
     int group, nblk;        // key heads of a group; blocks of rows of a head
-    int parts;              // workgroups that share the walk of a block of keys
+    int parts;              // workgroups that share the walk of a block
 };
 struct Place {
-    int kv, g, rank;        // g: the query head of the key head's, or the part
+    int kv, g, part, rank;      // key head, query head of it, part, block
 };
 template <bool PER_KEY_HEAD>
 __device__ __forceinline__ bool place(const Order& o, Place& p) {
-    const unsigned per = (unsigned)o.group * (unsigned)(PER_KEY_HEAD ? o.parts : o.G);
+    const unsigned heads = PER_KEY_HEAD ? 1u : (unsigned)o.G, per = (unsigned)o.group * heads * (unsigned)o.parts;
     const unsigned row = blockIdx.x / per, x = blockIdx.x - row * per;
-    const unsigned z = row / (unsigned)o.nblk;
+    const unsigned z = row / (unsigned)o.nblk, y = x / (unsigned)o.group;
     p.rank = (int)(row - z * (unsigned)o.nblk);
-    p.g = (int)(x / (unsigned)o.group);
+    p.part = (int)(y / heads);
+    p.g = (int)(y - (unsigned)p.part * heads);
     p.kv = (int)(z * (unsigned)o.group + x % (unsigned)o.group);
     return p.kv < o.BHk;
 }
@@ -221,8 +222,10 @@ struct FwdShared {
 template <int HD, int OWN, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
                                                       const bf16_t* __restrict__ V, const float* __restrict__ slopes,
-                                                      bf16_t* __restrict__ O, float* __restrict__ L, Order order, Rows rows, Score sc) {
+                                                      bf16_t* __restrict__ O, float* __restrict__ L, float4* __restrict__ sums,
+                                                      float2* __restrict__ stat, Order order, Rows rows, Score sc) {
     constexpr int NI = OWN / 32, NK = HD / 16, NV = HD / 32, WG = 4 * OWN;
+    static_assert(NI == 1, "a wave's 32 queries (the parts' layout)");
     constexpr bool RAW = !CAP && !BIAS;     // the products themselves are compared, and scaled with the subtraction
     __shared__ FwdShared<HD> sm;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, h = lane >> 5;
@@ -258,7 +261,12 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
     if (tid == 0) sm.found = 0;
     __syncthreads();
     Ends all = join(join(sm.ends[0], sm.ends[1]), join(sm.ends[2], sm.ends[3]));
-    const int t_lo = __builtin_amdgcn_readfirstlane(all.lo_min) / AT, t_hi = (__builtin_amdgcn_readfirstlane(all.hi_max) + AT - 1) / AT;
+    int t_lo = __builtin_amdgcn_readfirstlane(all.lo_min) / AT, t_hi = (__builtin_amdgcn_readfirstlane(all.hi_max) + AT - 1) / AT;
+    if (order.parts > 1) {          // (a part's tiles follow one another)
+        const int n = max(t_hi - t_lo, 0), first = t_lo;
+        t_lo = first + (int)((long long)n * at.part / order.parts);
+        t_hi = first + (int)((long long)n * (at.part + 1) / order.parts);
+    }
 
     const Reads<HD> rd(lane);
     auto tile = [&](int buf, int key0, bool masked) {
@@ -383,6 +391,18 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
             }
         }
     }
+    if (order.parts > 1) {
+        const size_t slot = (((size_t)at.part * order.BHk * order.G + (size_t)at.kv * order.G + at.g) * order.nblk + at.rank) * 4 + w;
+        float4* to = sums + slot * (4 * NV * 64) + lane;
+#pragma unroll
+        for (int vb = 0; vb < NV; ++vb)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                to[(4 * vb + k) * 64] = make_float4(acc[vb][0][4 * k], acc[vb][0][4 * k + 1], acc[vb][0][4 * k + 2], acc[vb][0][4 * k + 3]);
+        const float z = xor32_sum(lsum[0]);
+        if (h == 0) stat[slot * 32 + r32] = make_float2(m[0], z);
+        return;
+    }
 #pragma unroll
     for (int ib = 0; ib < NI; ++ib) {
         const int i = q0 + 32 * ib + r32;
@@ -393,6 +413,42 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
         for (int vb = 0; vb < NV; ++vb) store_block(O + row * HD + 32 * vb, acc[vb][ib], f, h, in);
         if (L != nullptr && h == 0 && in) L[row] = z != 0.f ? (m[ib] + __builtin_amdgcn_logf(z)) * LN2 : NEG_INF;
     }
+}
+
+// A block's rows from its parts, 32 values of each (blockIdx.y).  Blocks are numbered as the parts' kernel does, from the last one on.
+template <int HD>
+__global__ __launch_bounds__(256) void k_exp_fwd_join(const float4* __restrict__ sums, const float2* __restrict__ stat, bf16_t* __restrict__ O,
+                                                      float* __restrict__ L, int blocks, int nblk, int parts, int T) {
+    constexpr int NV = HD / 32;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r32 = lane & 31, h = lane >> 5, vb = (int)blockIdx.y;
+    const int head = (int)(blockIdx.x / (unsigned)nblk), rank = (int)(blockIdx.x - (unsigned)head * (unsigned)nblk);
+    const int i = (nblk - 1 - rank) * 128 + 32 * w + r32;
+    if (i >= T) return;
+    const size_t slot = (size_t)blockIdx.x * 4 + w, step = (size_t)blocks * 4;
+    float top = NEG_INF;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, stat[(slot + p * step) * 32 + r32].x);
+    float z = 0.f;
+    float4 x[4] = {};
+#pragma unroll 2
+    for (int p = 0; p < parts; ++p) {
+        const float2 s = stat[(slot + p * step) * 32 + r32];
+        // (a part without a weight adds nothing; one of NaN, whose reference may never have moved, all of it)
+        const float f = s.x == NEG_INF ? (s.y == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(s.x - top);
+        z += f * s.y;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float4 v = sums[(slot + p * step) * (4 * NV * 64) + (4 * vb + k) * 64 + lane];
+            x[k].x += f * v.x; x[k].y += f * v.y; x[k].z += f * v.z; x[k].w += f * v.w;
+        }
+    }
+    const float f = z != 0.f ? 1.f / z : 0.f;
+    const size_t row = (size_t)head * T + i;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bf16x4 o = {(__bf16)(x[k].x * f), (__bf16)(x[k].y * f), (__bf16)(x[k].z * f), (__bf16)(x[k].w * f)};
+        *(bf16x4*)(O + row * HD + 32 * vb + 8 * k + 4 * h) = o;
+    }
+    if (L != nullptr && vb == 0 && h == 0) L[row] = z != 0.f ? (top + __builtin_amdgcn_logf(z)) * LN2 : NEG_INF;
 }
 
 // ---- backward: preparation --------------------------------------------------------------------------------
@@ -725,7 +781,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
             }
             const int t = base + __builtin_ctzll(left);
             left &= left - 1;
-            const bool mine = turn == at.g;
+            const bool mine = turn == at.part;
             turn = turn + 1 == order.parts ? 0 : turn + 1;
             if (mine) return t;
         }
@@ -812,7 +868,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
     }
     if (order.parts > 1) {
         static_assert(NJ == 1, "a wave's 32 keys");
-        float4* to = sums + ((((size_t)at.g * order.BHk + at.kv) * order.nblk + at.rank) * 4 + w) * (8 * NF * 64) + lane;
+        float4* to = sums + ((((size_t)at.part * order.BHk + at.kv) * order.nblk + at.rank) * 4 + w) * (8 * NF * 64) + lane;
 #pragma unroll
         for (int fb = 0; fb < NF; ++fb)
 #pragma unroll
@@ -874,7 +930,7 @@ Order order_of(const pa_exp_problem& pr, int rows_per_block, int len) {
     return o;
 }
 long long blocks_of(const Order& o, bool per_key_head) {
-    return (long long)((o.BHk + o.group - 1) / o.group) * o.group * (per_key_head ? o.parts : o.G) * o.nblk;
+    return (long long)((o.BHk + o.group - 1) / o.group) * o.group * (per_key_head ? 1 : o.G) * o.parts * o.nblk;
 }
 
 template <int HD>
@@ -882,14 +938,41 @@ struct Shape {
     static constexpr int FWD_OWN = 32, FWD_WPE = 2, DQ_WPE = 2, DKDV_WPE = HD == 128 ? 1 : 2;
 };
 
+// Workgroups per block of 128 queries: until there are two per CU, as long as each has 8 tiles or more of those that the block may have
+// to walk.  (us, whole and in parts with their join: T1024 of Tk8192, H16/4 d128 capped, 128 blocks, 223 and 104 + 10 in four.  With
+// four per CU, 384 blocks of B2 H12 T4095 d64 take 52 + 15 in three parts, 65 whole.)
+int fwd_parts(const pa_exp_problem& pr, bool intervals) {
+    const Order o = order_of(pr, 128, pr.T);
+    const long long jobs = (long long)o.BHk * o.G * o.nblk;
+    const long long keys = pr.window > 0 && !intervals ? std::min<long long>(pr.Tk, 127LL + pr.window) : pr.Tk;
+    return (int)std::max(1LL, std::min({(512 + jobs - 1) / jobs, (keys + AT - 1) / AT / 8, 32LL}));
+}
+struct FwdParts {
+    size_t sums, stat;      // bytes
+};
+FwdParts fwd_part_bytes(const pa_exp_problem& pr, int parts) {
+    const Order o = order_of(pr, 128, pr.T);
+    const size_t rows = parts > 1 ? (size_t)parts * o.BHk * o.G * o.nblk * 128 : 0;
+    return {rows * pr.d * sizeof(float), rows * sizeof(float2)};
+}
 template <int HD, bool CAP, bool BIAS>
 pa_status fwd_t(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const ExpMask& mk, const Rows& rows, bf16_t* O,
-                float* L, hipStream_t s) {
+                float* L, char* ws, hipStream_t s) {
     constexpr int OWN = Shape<HD>::FWD_OWN;
-    const Order o = order_of(pr, 4 * OWN, pr.T);
-    LaunchScope ls("exp_fwd", s);
-    hipLaunchKernelGGL((k_exp_fwd<HD, OWN, Shape<HD>::FWD_WPE, CAP, BIAS>), dim3((unsigned)blocks_of(o, false)), dim3(256), 0, s, Q, K, V,
-                       mk.slopes, O, L, o, rows, score_of(pr));
+    Order o = order_of(pr, 4 * OWN, pr.T);
+    o.parts = fwd_parts(pr, rows.hi != nullptr);
+    float4* sums = (float4*)ws;
+    float2* stat = (float2*)(ws + fwd_part_bytes(pr, o.parts).sums);
+    {
+        LaunchScope ls("exp_fwd", s);
+        hipLaunchKernelGGL((k_exp_fwd<HD, OWN, Shape<HD>::FWD_WPE, CAP, BIAS>), dim3((unsigned)blocks_of(o, false)), dim3(256), 0, s, Q, K, V,
+                           mk.slopes, O, L, sums, stat, o, rows, score_of(pr));
+        if (!launch_ok()) return PA_ERR_HIP;
+    }
+    if (o.parts == 1) return PA_OK;
+    const int blocks = o.BHk * o.G * o.nblk;
+    LaunchScope ls("exp_fwd_join", s);
+    hipLaunchKernelGGL((k_exp_fwd_join<HD>), dim3((unsigned)blocks, HD / 32), dim3(256), 0, s, sums, stat, O, L, blocks, o.nblk, o.parts, pr.T);
     return launch_ok() ? PA_OK : PA_ERR_HIP;
 }
 // Workgroups per block of 128 keys: until there are four per CU, as long as each has 16 tiles or more.  (us, dK/dV and join, one and
@@ -974,15 +1057,19 @@ bool exp_grid_ok(const pa_exp_problem& pr) {
 }
 
 size_t exp_workspace_bytes(const pa_exp_problem& pr, bool backward) {
-    if (!backward) return 0;
+    if (!backward) {
+        // (whether a call brings intervals is not known here; without them it may take fewer parts, never more)
+        const FwdParts p = fwd_part_bytes(pr, fwd_parts(pr, true));
+        return align_up(p.sums + p.stat, 256);
+    }
     const BwdScratch sc = bwd_scratch(pr, nullptr);
     return (size_t)(char*)sc.ends + align_up((size_t)pr.B * ((pr.T + AT - 1) / AT) * sizeof(int4), 256) + part_bytes(pr);
 }
 
-pa_status exp_fwd(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, const bf16_t* V, ExpMask mk, bf16_t* O, float* L, char*,
+pa_status exp_fwd(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, const bf16_t* V, ExpMask mk, bf16_t* O, float* L, char* ws,
                   hipStream_t s) {
     return dispatch(pr, mk, [&](auto hd, auto cap, auto bias) {
-        return fwd_t<decltype(hd)::value, decltype(cap)::value, decltype(bias)::value>(pr, Q, K, V, mk, rows_of(pr, mk), O, L, s);
+        return fwd_t<decltype(hd)::value, decltype(cap)::value, decltype(bias)::value>(pr, Q, K, V, mk, rows_of(pr, mk), O, L, ws, s);
     });
 }
 

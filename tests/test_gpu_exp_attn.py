@@ -105,6 +105,22 @@ def test_documents_prefixes_and_padding(d, prefix, padding):
     both(q, k, v, g, scale=d ** -0.5, lo=lo, hi=hi, window=17, cap=5.0)
 
 
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_walks_shared_by_several_workgroups(d):
+    """Few blocks with long walks: keys in parts, rows of many heads in parts, rows that no part sees, a NaN in a masked place."""
+    q, k, v, g = make(1, 8, 1, 600, 1100, d, seed=d)
+    both(q, k, v, g, scale=d ** -0.5, cap=6.0)
+    lo, hi = documents(1, 600, 2, padding=70)
+    q, k, v, g = make(1, 16, 2, 600, 600, d, seed=d + 1)
+    want = exp_attn(q, k, v, g=g, scale=d ** -0.5, lo=lo, hi=hi)
+    for x in (q, k, v, g):
+        x[:, :, 530:] = math.nan
+    check(run(q, k, v, g, scale=d ** -0.5, row_lo=lo, row_hi=hi), want)
+    q, k, v, g = make(1, 2, 1, 3, 2100, d, seed=d + 2)
+    both(q, k, v, g, scale=d ** -0.5, window=1500)
+    both(q, k, v, g, scale=d ** -0.5, hi=torch.tensor([[0, 2100, 700]], dtype=torch.int32), lo=torch.tensor([[0, 40, 699]], dtype=torch.int32))
+
+
 def test_every_key_seen_and_none():
     q, k, v, g = make(2, 2, 2, 100, 180, 64, seed=5)
     full = torch.full((2, 100), 180, dtype=torch.int32)
