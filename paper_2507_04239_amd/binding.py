@@ -476,6 +476,8 @@ def power_attn_exp_workspace_bytes(prob: PaExpProblem, for_backward: bool) -> in
 
 
 def _exp_masks(Q, slopes, row_lo, row_hi):
+    if slopes is None and row_lo is None and row_hi is None:
+        return None, None, None
     import torch
     B, H, T, _ = Q.shape
     return (_array_ptr(slopes, Q, (H,), torch.float32, "slopes"), _array_ptr(row_lo, Q, (B, T), torch.int32, "row_lo"),
@@ -496,12 +498,13 @@ def power_attn_exp_fwd(Q, K, V, scale: float = 1.0, cap: float = 0.0, window: in
     masks = _exp_masks(Q, slopes, row_lo, row_hi)
     with _OnDevice(Q.device):
         O = torch.empty_like(Q) if out is None else out
-        L = torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device) if out_lse is None else out_lse
+        L = Q.new_empty(Q.shape[:3], dtype=torch.float32) if out_lse is None else out_lse
+        o = O.data_ptr() if out is None else _shaped_ptr(O, Q, Q.shape, "O")
+        l = L.data_ptr() if out_lse is None else _array_ptr(L, Q, Q.shape[:3], torch.float32, "L")
         ws = 0
         if need > 0:
             workspace, ws = _workspace(need, workspace, Q.device)
-        st = lib.power_attn_exp_fwd(prob, q, k, v, *masks, _shaped_ptr(O, Q, Q.shape, "O"),
-                                    _array_ptr(L, Q, Q.shape[:3], torch.float32, "L"), ws, need, _stream())
+        st = lib.power_attn_exp_fwd(prob, q, k, v, *masks, o, l, ws, need, _stream())
     if st != 0:
         _check(lib, st, "power_attn_exp_fwd")
     return O, L
@@ -542,10 +545,19 @@ def power_attn_cache_step_workspace_bytes(cache: PaCache) -> int:
     return int(load_library().power_attn_cache_step_workspace_bytes(ctypes.byref(cache)))
 
 
-def _cache_ptrs(lib, cache, pool, table, what):
+# (by the values of the struct's fields)
+@functools.lru_cache(maxsize=512)
+def _cache_plan(fields: bytes):
+    """-> bytes of the pool, bytes of a step's workspace"""
+    lib = load_library()
+    ref = ctypes.byref(PaCache.from_buffer_copy(fields))
+    return int(lib.power_attn_cache_bytes(ref)), int(lib.power_attn_cache_step_workspace_bytes(ref))
+
+
+def _cache_ptrs(cache, pool, table, what):
     """Pointers of pool and table, which must be as large as the cache says"""
     import torch
-    need = int(lib.power_attn_cache_bytes(ctypes.byref(cache)))
+    need = _cache_plan(bytes(cache))[0]
     if need == 0:
         raise PowerAttnError(f"{what}: invalid or unsupported cache")
     if pool.numel() * pool.element_size() < need:
@@ -574,7 +586,7 @@ def power_attn_cache_append(cache: PaCache, K, V, pool, table, past, count=None,
         raise PowerAttnError("power_attn_cache_append: K and V, Q, or all of them")
     T = (K if K is not None else Q).shape[2]
     with _OnDevice(pool.device):
-        p, t = _cache_ptrs(lib, cache, pool, table, "power_attn_cache_append")
+        p, t = _cache_ptrs(cache, pool, table, "power_attn_cache_append")
         k = v = q = qo = c = s = None
         if K is not None:
             k, v = _rows_ptr(K, pool, cache, cache.Hk, T, "K"), _rows_ptr(V, pool, cache, cache.Hk, T, "V")
@@ -598,7 +610,7 @@ def power_attn_cache_read(cache: PaCache, pool, table, start, T: int, count=None
     import torch
     lib = load_library()
     with _OnDevice(pool.device):
-        p, t = _cache_ptrs(lib, cache, pool, table, "power_attn_cache_read")
+        p, t = _cache_ptrs(cache, pool, table, "power_attn_cache_read")
         K, V = out if out is not None else (torch.empty(cache.B, cache.Hk, T, cache.d, dtype=torch.bfloat16, device=pool.device)
                                             for _ in range(2))
         st = lib.power_attn_cache_read(cache, T, p, t, _lengths_ptr(start, pool, cache, "start"), _lengths_ptr(count, pool, cache, "count"),
@@ -615,10 +627,10 @@ def power_attn_cache_step(cache: PaCache, q, pool, table, lens, slopes=None, out
     if q.dtype is not torch.bfloat16 or q.device != pool.device or tuple(q.shape) != (cache.B, cache.H, cache.d):
         raise PowerAttnError(f"q must be bfloat16 {[cache.B, cache.H, cache.d]} on the pool's device")
     with _OnDevice(pool.device):
-        p, t = _cache_ptrs(lib, cache, pool, table, "power_attn_cache_step")
+        p, t = _cache_ptrs(cache, pool, table, "power_attn_cache_step")
         o = torch.empty_like(q) if out is None else out
         L = torch.empty(cache.B, cache.H, dtype=torch.float32, device=pool.device) if out_lse is None else out_lse
-        need = int(lib.power_attn_cache_step_workspace_bytes(cache))
+        need = _cache_plan(bytes(cache))[1]
         workspace, ws = _workspace(need, workspace, pool.device)
         st = lib.power_attn_cache_step(cache, _dev_ptr(q, name="q"), _array_ptr(slopes, q, (cache.H,), torch.float32, "slopes"), p, t,
                                        _lengths_ptr(lens, pool, cache, "lens"), _shaped_ptr(o, q, q.shape, "o"),

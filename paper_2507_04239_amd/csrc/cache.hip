@@ -398,19 +398,7 @@ __device__ __forceinline__ Visible visible(const int* lens, int b, int B, const 
     }
     return v;
 }
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) x += __shfl_xor(x, off);
-    return __builtin_amdgcn_readfirstlane(x);
-}
-__device__ __forceinline__ int wave_scan(int x, int lane) {     // inclusive
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        if (lane >= off) x += y;
-    }
-    return x;
-}
+__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 // (the units of all sequences together number less than 2^31)
 __device__ __forceinline__ int total_units(const int* lens, int B, const Pages& pg, int window, int lane) {
     int total = 0;
@@ -775,7 +763,7 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     int before = 0;
     for (int base = 0; base < B && before < end; base += 64) {
         const Visible v = visible(lens, base + lane, B, pg, window);
-        const int upto = before + wave_scan(v.units, lane);
+        const int upto = before + wave_scan(v.units);
         uint64_t mine = __ballot(v.units > 0 && upto > begin && upto - v.units < end);
         for (; mine != 0; mine &= mine - 1) {
             const int at = __builtin_ctzll(mine);

@@ -75,18 +75,15 @@ struct Ends {
 __device__ __forceinline__ Ends join(const Ends& a, const Ends& b) {
     return {min(a.lo_min, b.lo_min), max(a.hi_max, b.hi_max), max(a.lo_max, b.lo_max), min(a.hi_min, b.hi_min)};
 }
+// (the halves of the wave hold the same rows, or are joined by BOTH)
+template <bool BOTH>
 __device__ __forceinline__ Ends wave_ends(Range r) {
-    Ends e{r.lo, r.hi, r.lo, r.hi};
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const Ends o{__shfl_xor(e.lo_min, off), __shfl_xor(e.hi_max, off), __shfl_xor(e.lo_max, off), __shfl_xor(e.hi_min, off)};
-        e = join(e, o);
-    }
-    e.lo_min = __builtin_amdgcn_readfirstlane(e.lo_min);
-    e.hi_max = __builtin_amdgcn_readfirstlane(e.hi_max);
-    e.lo_max = __builtin_amdgcn_readfirstlane(e.lo_max);
-    e.hi_min = __builtin_amdgcn_readfirstlane(e.hi_min);
-    return e;
+    Ends e{half_min(r.lo), half_max(r.hi), half_max(r.lo), half_min(r.hi)};
+    if (BOTH)
+        e = join(e, {__builtin_amdgcn_readlane(e.lo_min, 32), __builtin_amdgcn_readlane(e.hi_max, 32),
+                     __builtin_amdgcn_readlane(e.lo_max, 32), __builtin_amdgcn_readlane(e.hi_min, 32)});
+    return {__builtin_amdgcn_readfirstlane(e.lo_min), __builtin_amdgcn_readfirstlane(e.hi_max), __builtin_amdgcn_readfirstlane(e.lo_max),
+            __builtin_amdgcn_readfirstlane(e.hi_min)};
 }
 
 // ---- the streamed tile ------------------------------------------------------------------------------------
@@ -249,7 +246,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
         lsum[ib] = 0.f;
         m[ib] = NEG_INF;
         rg[ib] = row_range(rows, b, i);
-        mine = join(mine, wave_ends(rg[ib]));
+        mine = join(mine, wave_ends<false>(rg[ib]));
 #pragma unroll
         for (int ks = 0; ks < NK; ++ks) qf[ib][ks] = row_frag_global<HD>(Q, row0 + i, ks, h);
 #pragma unroll
@@ -484,7 +481,7 @@ __global__ __launch_bounds__(256) void k_exp_prep(const bf16_t* __restrict__ dO,
     const int i = t * AT + tid;
     const Range r = i < rows.T ? row_range(rows, b, i) : Range{rows.Tk, 0};
     if (i < rows.T) to.range[(size_t)b * rows.T + i] = make_int2(r.lo, r.hi);
-    const Ends e = wave_ends(r);
+    const Ends e = wave_ends<true>(r);
     if (tid == 0) to.ends[(size_t)b * ntile + t] = make_int4(e.lo_min, e.hi_max, e.lo_max, e.hi_min);
 }
 
@@ -533,7 +530,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
         const int i = min(q0 + 32 * ib + r32, rows.T - 1);
         st[ib] = stat[row0 + i];
         rg[ib] = row_range(rows, b, i);
-        mine = join(mine, wave_ends(rg[ib]));
+        mine = join(mine, wave_ends<false>(rg[ib]));
 #pragma unroll
         for (int ks = 0; ks < NK; ++ks) {
             qf[ib][ks] = row_frag_global<HD>(Q, row0 + i, ks, h);

@@ -131,6 +131,32 @@ __device__ __forceinline__ float xor32_sum(float x) {
     return lo + hi;
 }
 
+// another lane's integer: DPP control words (gfx9): quad permutations, mirrors inside a row of 16 lanes, shifts and broadcasts over rows
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int dpp(int x, int old) {
+    return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xf, false);
+}
+// least / greatest of 32 lanes, in each of them
+__device__ __forceinline__ int half_min(int x) {
+    x = min(x, dpp<0xB1>(x, x));        // lane ^ 1
+    x = min(x, dpp<0x4E>(x, x));        // lane ^ 2
+    x = min(x, dpp<0x141>(x, x));       // the other quad of 8 lanes
+    x = min(x, dpp<0x140>(x, x));       // the other 8 of 16
+    const auto r = __builtin_amdgcn_permlane16_swap((unsigned)x, (unsigned)x, false, false);
+    return min((int)r[0], (int)r[1]);
+}
+__device__ __forceinline__ int half_max(int x) { return ~half_min(~x); }
+// sums of lanes 0 .. l
+__device__ __forceinline__ int wave_scan(int x) {
+    x += dpp<0x111>(x, 0);              // 1, 2, 4, 8 lanes down inside a row
+    x += dpp<0x112>(x, 0);
+    x += dpp<0x114>(x, 0);
+    x += dpp<0x118>(x, 0);
+    x += dpp<0x142, 0xa>(x, 0);         // the last lane of a row to the next one (rows 1 and 3)
+    x += dpp<0x143, 0xc>(x, 0);         // lane 31 to rows 2 and 3
+    return x;
+}
+
 // ---- launchers (each defined next to its kernels) ------------------------------------------
 
 // ---- resident-state kernels (chunk states kept in registers; see mfma_resident.hip) ----------------
