@@ -443,28 +443,28 @@ def _exp_plan(for_backward, B, H, Hk, T, Tk, d, scale, cap, window, dtype):
     return ref, int(lib.power_attn_exp_supported(ref, for_backward)), int(lib.power_attn_exp_workspace_bytes(ref, for_backward))
 
 
-def _exp_plan_of(for_backward, Q, K, V, scale, cap, window):
-    if Q.dim() != 4 or K.dim() != 4:
-        raise PowerAttnError("tensors must be [B, H, T, d]")
-    B, H, T, d = Q.shape
-    if K.shape[0] != B or K.shape[3] != d or K.shape != V.shape:
-        raise PowerAttnError("K and V must be [B, Hk, Tk, d] of Q's B and d")
-    return _exp_plan(for_backward, B, H, K.shape[1], T, K.shape[2], d, float(scale), float(cap), operator.index(window), _dtype_name(Q))
-
-
-def _array_ptr(t, like, shape, dtype, name):
-    """Device pointer of an optional contiguous array on `like`'s device"""
-    if t is None:
-        return None
-    if t.device != like.device or not t.is_contiguous() or t.dtype is not dtype or tuple(t.shape) != tuple(shape):
-        raise PowerAttnError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on the device of the others")
+def _tensor_ptr(t, index, dtype, shape, name):
+    """Device pointer of a contiguous tensor of that type and shape on GPU `index`"""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise PowerAttnError(f"{name} must be a contiguous {dtype} tensor {list(shape)} on the GPU of the others, "
+                             f"not {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _shaped_ptr(t, like, shape, name):
-    if tuple(t.shape) != tuple(shape):
-        raise PowerAttnError(f"{name} must be {list(shape)}")
-    return _dev_ptr(t, like, name)
+def _optional_ptr(t, index, dtype, shape, name):
+    return None if t is None else _tensor_ptr(t, index, dtype, shape, name)
+
+
+def _launch(fn, index, what, *args):
+    """fn(*args, the current stream of GPU `index`), with that GPU the current one"""
+    import torch
+    if torch._C._cuda_getDevice() == index:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if st != 0:
+        _check(load_library(), st, what)
 
 
 def power_attn_exp_supported(prob: PaExpProblem, for_backward: bool) -> bool:
@@ -475,13 +475,26 @@ def power_attn_exp_workspace_bytes(prob: PaExpProblem, for_backward: bool) -> in
     return int(load_library().power_attn_exp_workspace_bytes(ctypes.byref(prob), int(for_backward)))
 
 
-def _exp_masks(Q, slopes, row_lo, row_hi):
-    if slopes is None and row_lo is None and row_hi is None:
-        return None, None, None
+def _exp_inputs(for_backward, what, Q, K, V, scale, cap, window, slopes, row_lo, row_hi):
+    """-> GPU, type, plan, pointers of Q, K, V and of the masks"""
     import torch
-    B, H, T, _ = Q.shape
-    return (_array_ptr(slopes, Q, (H,), torch.float32, "slopes"), _array_ptr(row_lo, Q, (B, T), torch.int32, "row_lo"),
-            _array_ptr(row_hi, Q, (B, T), torch.int32, "row_hi"))
+    if Q.dim() != 4 or K.dim() != 4:
+        raise PowerAttnError("tensors must be [B, H, T, d]")
+    shape, kv, index, dtype = Q.shape, K.shape, Q.get_device(), Q.dtype
+    if index < 0:
+        raise PowerAttnError("Q must be on the GPU")
+    B, H, T, d = shape
+    if kv[0] != B or kv[3] != d:
+        raise PowerAttnError("K and V must be [B, Hk, Tk, d] of Q's B and d")
+    plan = _exp_plan(for_backward, B, H, kv[1], T, kv[2], d, float(scale), float(cap), operator.index(window), _dtype_name(Q))
+    if plan[1] != 0:
+        _check(load_library(), plan[1], what)
+    ptrs = (_tensor_ptr(Q, index, dtype, shape, "Q"), _tensor_ptr(K, index, dtype, kv, "K"), _tensor_ptr(V, index, dtype, kv, "V"))
+    if slopes is None and row_lo is None and row_hi is None:
+        return index, dtype, plan, ptrs, (None, None, None)
+    return index, dtype, plan, ptrs, (_optional_ptr(slopes, index, torch.float32, (H,), "slopes"),
+                                      _optional_ptr(row_lo, index, torch.int32, (B, T), "row_lo"),
+                                      _optional_ptr(row_hi, index, torch.int32, (B, T), "row_hi"))
 
 
 def power_attn_exp_fwd(Q, K, V, scale: float = 1.0, cap: float = 0.0, window: int = 0, slopes=None, row_lo=None, row_hi=None,
@@ -490,23 +503,15 @@ def power_attn_exp_fwd(Q, K, V, scale: float = 1.0, cap: float = 0.0, window: in
     cap > 0 caps the scores by cap tanh(x / cap); slopes (float32 [H]) subtracts slope |pos - j|; row i sees the keys row_lo[b, i]
     <= j < row_hi[b, i] (int32 [B, T]; without them all up to its position i + Tk - T) of the last `window`, if one is given."""
     import torch
-    lib = load_library()
-    q, k, v = _dev_ptr(Q, None, "Q"), _dev_ptr(K, Q, "K"), _dev_ptr(V, Q, "V")
-    prob, status, need = _exp_plan_of(0, Q, K, V, scale, cap, window)
-    if status != 0:
-        _check(lib, status, "power_attn_exp_fwd")
-    masks = _exp_masks(Q, slopes, row_lo, row_hi)
-    with _OnDevice(Q.device):
-        O = torch.empty_like(Q) if out is None else out
-        L = Q.new_empty(Q.shape[:3], dtype=torch.float32) if out_lse is None else out_lse
-        o = O.data_ptr() if out is None else _shaped_ptr(O, Q, Q.shape, "O")
-        l = L.data_ptr() if out_lse is None else _array_ptr(L, Q, Q.shape[:3], torch.float32, "L")
-        ws = 0
-        if need > 0:
-            workspace, ws = _workspace(need, workspace, Q.device)
-        st = lib.power_attn_exp_fwd(prob, q, k, v, *masks, o, l, ws, need, _stream())
-    if st != 0:
-        _check(lib, st, "power_attn_exp_fwd")
+    index, dtype, (prob, _, need), qkv, masks = _exp_inputs(0, "power_attn_exp_fwd", Q, K, V, scale, cap, window, slopes, row_lo, row_hi)
+    O = torch.empty_like(Q) if out is None else out
+    L = Q.new_empty(Q.shape[:3], dtype=torch.float32) if out_lse is None else out_lse
+    o = O.data_ptr() if out is None else _tensor_ptr(O, index, dtype, Q.shape, "O")
+    l = L.data_ptr() if out_lse is None else _tensor_ptr(L, index, torch.float32, Q.shape[:3], "L")
+    ws = None
+    if need > 0:
+        workspace, ws = _workspace(need, workspace, Q.device)
+    _launch(load_library().power_attn_exp_fwd, index, "power_attn_exp_fwd", prob, *qkv, *masks, o, l, ws, need)
     return O, L
 
 
@@ -514,20 +519,14 @@ def power_attn_exp_bwd(Q, K, V, O, L, dO, scale: float = 1.0, cap: float = 0.0, 
                        workspace=None, out=None):
     """Backward pass of power_attn_exp_fwd on the current stream: its O and L, and dO -> (dQ, dK, dV)."""
     import torch
-    lib = load_library()
-    q, k, v, g = _dev_ptr(Q, None, "Q"), _dev_ptr(K, Q, "K"), _dev_ptr(V, Q, "V"), _shaped_ptr(dO, Q, Q.shape, "dO")
-    prob, status, need = _exp_plan_of(1, Q, K, V, scale, cap, window)
-    if status != 0:
-        _check(lib, status, "power_attn_exp_bwd")
-    masks = _exp_masks(Q, slopes, row_lo, row_hi)
-    with _OnDevice(Q.device):
-        dQ, dK, dV = (torch.empty_like(x) for x in (Q, K, V)) if out is None else out
-        workspace, ws = _workspace(need, workspace, Q.device)
-        st = lib.power_attn_exp_bwd(prob, q, k, v, *masks, _shaped_ptr(O, Q, Q.shape, "O"), _array_ptr(L, Q, Q.shape[:3], torch.float32, "L"),
-                                    g, _shaped_ptr(dQ, Q, Q.shape, "dQ"), _shaped_ptr(dK, Q, K.shape, "dK"),
-                                    _shaped_ptr(dV, Q, K.shape, "dV"), ws, need, _stream())
-    if st != 0:
-        _check(lib, st, "power_attn_exp_bwd")
+    index, dtype, (prob, _, need), qkv, masks = _exp_inputs(1, "power_attn_exp_bwd", Q, K, V, scale, cap, window, slopes, row_lo, row_hi)
+    rest = (_tensor_ptr(O, index, dtype, Q.shape, "O"), _tensor_ptr(L, index, torch.float32, Q.shape[:3], "L"),
+            _tensor_ptr(dO, index, dtype, Q.shape, "dO"))
+    dQ, dK, dV = (torch.empty_like(x) for x in (Q, K, V)) if out is None else out
+    grads = (_tensor_ptr(dQ, index, dtype, Q.shape, "dQ"), _tensor_ptr(dK, index, dtype, K.shape, "dK"),
+             _tensor_ptr(dV, index, dtype, K.shape, "dV"))
+    workspace, ws = _workspace(need, workspace, Q.device)
+    _launch(load_library().power_attn_exp_bwd, index, "power_attn_exp_bwd", prob, *qkv, *masks, *rest, *grads, ws, need)
     return dQ, dK, dV
 
 
@@ -537,70 +536,62 @@ def make_cache(B, H, Hk, d, page, max_pages, num_pages, bits=16, rot=0, rot_adja
     return PaCache(B, H, Hk, d, page, max_pages, num_pages, bits, rot, int(bool(rot_adjacent)), rot_rows, float(scale), float(cap), int(window))
 
 
+# What the library says about a cache depends on its fields alone (bytes(cache): by their values).
+@functools.lru_cache(maxsize=512)
+def _cache_plan(fields: bytes):
+    """-> pointer to the struct, its B, H, Hk and d, bytes of the pool and of a step's workspace, the table's shape"""
+    lib = load_library()
+    c = PaCache.from_buffer_copy(fields)
+    ref = ctypes.pointer(c)
+    return (ref, c.B, c.H, c.Hk, c.d, int(lib.power_attn_cache_bytes(ref)), int(lib.power_attn_cache_step_workspace_bytes(ref)),
+            (c.B, c.max_pages))
+
+
 def power_attn_cache_bytes(cache: PaCache) -> int:
-    return int(load_library().power_attn_cache_bytes(ctypes.byref(cache)))
+    return _cache_plan(bytes(cache))[5]
 
 
 def power_attn_cache_step_workspace_bytes(cache: PaCache) -> int:
-    return int(load_library().power_attn_cache_step_workspace_bytes(ctypes.byref(cache)))
+    return _cache_plan(bytes(cache))[6]
 
 
-# (by the values of the struct's fields)
-@functools.lru_cache(maxsize=512)
-def _cache_plan(fields: bytes):
-    """-> bytes of the pool, bytes of a step's workspace"""
-    lib = load_library()
-    ref = ctypes.byref(PaCache.from_buffer_copy(fields))
-    return int(lib.power_attn_cache_bytes(ref)), int(lib.power_attn_cache_step_workspace_bytes(ref))
-
-
-def _cache_ptrs(cache, pool, table, what):
-    """Pointers of pool and table, which must be as large as the cache says"""
+def _cache_inputs(cache, pool, table, what):
+    """-> plan, GPU, pointers of pool (which must be as large as the cache says) and table"""
     import torch
-    need = _cache_plan(bytes(cache))[0]
+    plan = _cache_plan(bytes(cache))
+    need, index = plan[5], pool.get_device()
     if need == 0:
         raise PowerAttnError(f"{what}: invalid or unsupported cache")
+    if index < 0 or not pool.is_contiguous():
+        raise PowerAttnError("pool must be contiguous and on the GPU")
     if pool.numel() * pool.element_size() < need:
         raise PowerAttnError(f"{what}: pool holds {pool.numel() * pool.element_size()} bytes, {need} needed")
-    return _dev_ptr(pool, name="pool"), _array_ptr(table, pool, (cache.B, cache.max_pages), torch.int32, "table")
-
-
-def _lengths_ptr(t, pool, cache, name):
-    import torch
-    return _array_ptr(t, pool, (cache.B,), torch.int32, name)
-
-
-def _rows_ptr(t, pool, cache, heads, T, name):
-    import torch
-    if t.dtype is not torch.bfloat16 or t.device != pool.device or tuple(t.shape) != (cache.B, heads, T, cache.d):
-        raise PowerAttnError(f"{name} must be bfloat16 {[cache.B, heads, T, cache.d]} on the pool's device")
-    return _dev_ptr(t, name=name)
+    return plan, index, pool.data_ptr(), _tensor_ptr(table, index, torch.int32, plan[7], "table")
 
 
 def power_attn_cache_append(cache: PaCache, K, V, pool, table, past, count=None, Q=None, cos=None, sin=None, out_q=None):
     """K, V [B, Hk, T, d] (or None) into the cache at positions past[b] + t, t < count[b], keys rotated by cos, sin (float32
     [rot_rows, rot / 2]) on the way; -> Q [B, H, T, d] rotated likewise, into out_q (which may be Q), or None without Q."""
     import torch
-    lib = load_library()
+    (ref, B, H, Hk, d, *_), index, p, t = _cache_inputs(cache, pool, table, "power_attn_cache_append")
     if (K is None) != (V is None) or (K is None and Q is None):
         raise PowerAttnError("power_attn_cache_append: K and V, Q, or all of them")
     T = (K if K is not None else Q).shape[2]
-    with _OnDevice(pool.device):
-        p, t = _cache_ptrs(cache, pool, table, "power_attn_cache_append")
-        k = v = q = qo = c = s = None
-        if K is not None:
-            k, v = _rows_ptr(K, pool, cache, cache.Hk, T, "K"), _rows_ptr(V, pool, cache, cache.Hk, T, "V")
-        if Q is not None:
-            q = _rows_ptr(Q, pool, cache, cache.H, T, "Q")
-            out_q = torch.empty_like(Q) if out_q is None else out_q
-            qo = _rows_ptr(out_q, pool, cache, cache.H, T, "out_q")
-        if cache.rot > 0:
-            shape = (cache.rot_rows, cache.rot // 2)
-            c, s = _array_ptr(cos, pool, shape, torch.float32, "cos"), _array_ptr(sin, pool, shape, torch.float32, "sin")
-        st = lib.power_attn_cache_append(cache, T, k, v, q, qo, c, s, p, t, _lengths_ptr(past, pool, cache, "past"),
-                                         _lengths_ptr(count, pool, cache, "count"), _stream())
-    if st != 0:
-        _check(lib, st, "power_attn_cache_append")
+    bf16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    k = v = q = qo = c = s = None
+    if K is not None:
+        k, v = _tensor_ptr(K, index, bf16, (B, Hk, T, d), "K"), _tensor_ptr(V, index, bf16, (B, Hk, T, d), "V")
+    if Q is not None:
+        q = _tensor_ptr(Q, index, bf16, (B, H, T, d), "Q")
+        out_q = torch.empty_like(Q) if out_q is None else out_q
+        qo = _tensor_ptr(out_q, index, bf16, (B, H, T, d), "out_q")
+    if cache.rot > 0:
+        if cos is None or sin is None:
+            raise PowerAttnError("power_attn_cache_append: a cache that rotates needs cos and sin")
+        shape = (cache.rot_rows, cache.rot // 2)
+        c, s = _tensor_ptr(cos, index, f32, shape, "cos"), _tensor_ptr(sin, index, f32, shape, "sin")
+    _launch(load_library().power_attn_cache_append, index, "power_attn_cache_append", ref, T, k, v, q, qo, c, s, p, t,
+            _tensor_ptr(past, index, i32, (B,), "past"), _optional_ptr(count, index, i32, (B,), "count"))
     return out_q if Q is not None else None
 
 
@@ -608,33 +599,24 @@ def power_attn_cache_read(cache: PaCache, pool, table, start, T: int, count=None
     """-> K, V [B, Hk, T, d] bfloat16: the values held at positions start[b] + t, t < count[b].  Rows that are not there are left as
     they are in `out`, and undefined without it."""
     import torch
-    lib = load_library()
-    with _OnDevice(pool.device):
-        p, t = _cache_ptrs(cache, pool, table, "power_attn_cache_read")
-        K, V = out if out is not None else (torch.empty(cache.B, cache.Hk, T, cache.d, dtype=torch.bfloat16, device=pool.device)
-                                            for _ in range(2))
-        st = lib.power_attn_cache_read(cache, T, p, t, _lengths_ptr(start, pool, cache, "start"), _lengths_ptr(count, pool, cache, "count"),
-                                       _rows_ptr(K, pool, cache, cache.Hk, T, "K"), _rows_ptr(V, pool, cache, cache.Hk, T, "V"), _stream())
-    if st != 0:
-        _check(lib, st, "power_attn_cache_read")
+    (ref, B, _, Hk, d, *_), index, p, t = _cache_inputs(cache, pool, table, "power_attn_cache_read")
+    bf16, i32, shape = torch.bfloat16, torch.int32, (B, Hk, operator.index(T), d)
+    K, V = out if out is not None else (torch.empty(shape, dtype=bf16, device=pool.device) for _ in range(2))
+    _launch(load_library().power_attn_cache_read, index, "power_attn_cache_read", ref, T, p, t, _tensor_ptr(start, index, i32, (B,), "start"),
+            _optional_ptr(count, index, i32, (B,), "count"), _tensor_ptr(K, index, bf16, shape, "K"), _tensor_ptr(V, index, bf16, shape, "V"))
     return K, V
 
 
 def power_attn_cache_step(cache: PaCache, q, pool, table, lens, slopes=None, out=None, out_lse=None, workspace=None):
     """One token for every sequence: q [B, H, d] (rotated), the last of the lens[b] tokens held -> (o [B, H, d], L [B, H] float32)."""
     import torch
-    lib = load_library()
-    if q.dtype is not torch.bfloat16 or q.device != pool.device or tuple(q.shape) != (cache.B, cache.H, cache.d):
-        raise PowerAttnError(f"q must be bfloat16 {[cache.B, cache.H, cache.d]} on the pool's device")
-    with _OnDevice(pool.device):
-        p, t = _cache_ptrs(cache, pool, table, "power_attn_cache_step")
-        o = torch.empty_like(q) if out is None else out
-        L = torch.empty(cache.B, cache.H, dtype=torch.float32, device=pool.device) if out_lse is None else out_lse
-        need = _cache_plan(bytes(cache))[1]
-        workspace, ws = _workspace(need, workspace, pool.device)
-        st = lib.power_attn_cache_step(cache, _dev_ptr(q, name="q"), _array_ptr(slopes, q, (cache.H,), torch.float32, "slopes"), p, t,
-                                       _lengths_ptr(lens, pool, cache, "lens"), _shaped_ptr(o, q, q.shape, "o"),
-                                       _array_ptr(L, pool, (cache.B, cache.H), torch.float32, "L"), ws, need, _stream())
-    if st != 0:
-        _check(lib, st, "power_attn_cache_step")
+    (ref, B, H, _, d, _, need, _), index, p, t = _cache_inputs(cache, pool, table, "power_attn_cache_step")
+    bf16, f32 = torch.bfloat16, torch.float32
+    qp = _tensor_ptr(q, index, bf16, (B, H, d), "q")
+    o = torch.empty_like(q) if out is None else out
+    L = q.new_empty((B, H), dtype=f32) if out_lse is None else out_lse
+    workspace, ws = _workspace(need, workspace, pool.device)
+    _launch(load_library().power_attn_cache_step, index, "power_attn_cache_step", ref, qp, _optional_ptr(slopes, index, f32, (H,), "slopes"),
+            p, t, _tensor_ptr(lens, index, torch.int32, (B,), "lens"), o.data_ptr() if out is None else _tensor_ptr(o, index, bf16, (B, H, d), "o"),
+            L.data_ptr() if out_lse is None else _tensor_ptr(L, index, f32, (B, H), "L"), ws, need)
     return o, L

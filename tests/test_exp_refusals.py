@@ -103,12 +103,29 @@ def test_cache_arguments(lib):
     assert lib.power_attn_cache_step(c, *step[:7], odd, need, None) == 3
 
 
-def test_binding_checks_shapes():
+def test_binding_checks_tensors():
     import torch
-    q, k = torch.zeros(1, 4, 5, 64), torch.zeros(1, 2, 5, 64)
+    q, k = torch.zeros(1, 4, 5, 64, dtype=torch.bfloat16), torch.zeros(1, 2, 5, 64, dtype=torch.bfloat16)
     with pytest.raises(pa.PowerAttnError, match="GPU"):
         pa.power_attn_exp_fwd(q, k, k)
+    with pytest.raises(pa.PowerAttnError, match="B, H, T, d"):
+        pa.power_attn_exp_fwd(q[0], k, k)
     with pytest.raises(pa.PowerAttnError):
-        pa._exp_plan_of(0, q, k, torch.zeros(1, 2, 6, 64), 1.0, 0.0, 0)
+        pa._tensor_ptr(q, -1, torch.bfloat16, (1, 4, 6, 64), "Q")
     with pytest.raises(pa.PowerAttnError):
-        pa._exp_plan_of(0, q, torch.zeros(1, 2, 5, 32), torch.zeros(1, 2, 5, 32), 1.0, 0.0, 0)
+        pa._tensor_ptr(q.float(), -1, torch.bfloat16, (1, 4, 5, 64), "Q")
+    with pytest.raises(pa.PowerAttnError):
+        pa._tensor_ptr(q.transpose(1, 2), -1, torch.bfloat16, (1, 5, 4, 64), "Q")
+    c = pa.make_cache(**CACHE)
+    pool = torch.zeros(pa.power_attn_cache_bytes(c), dtype=torch.uint8)
+    with pytest.raises(pa.PowerAttnError, match="GPU"):
+        pa.power_attn_cache_step(c, q[:, :, 0], pool, torch.zeros(2, 4, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(pa.PowerAttnError, match="unsupported"):
+        pa.power_attn_cache_read(pa.make_cache(**{**CACHE, "d": 32}), pool, None, None, 1)
+
+
+def test_plans_of_a_cache_follow_its_fields():
+    c = pa.make_cache(**CACHE)
+    before = pa.power_attn_cache_bytes(c)
+    c.num_pages *= 2
+    assert pa.power_attn_cache_bytes(c) == 2 * before
