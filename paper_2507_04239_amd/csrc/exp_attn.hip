@@ -24,6 +24,7 @@ namespace {
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float NEG_INF = -__builtin_inff();
+constexpr int BLOCK = 128;      // rows that a workgroup owns, 32 a wave
 
 // ---- the score --------------------------------------------------------------------------------------
 // cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1): one exponential and one reciprocal, exact at both ends (exp 0 and
@@ -157,16 +158,17 @@ __device__ __forceinline__ bf16x8 col_op(uint32_t tile, const Reads<HD>& rd, int
     return f.v;
 }
 
-// Infinities and NaN of rows that are masked for some row of the other side must not reach it, and in a matrix product they would
-// (0 x NaN).  So in tiles that are not seen whole by the whole workgroup such values are replaced by zeros.  Where there
-// were any, a second walk over those tiles adds what the pairs that are seen would have received.
+// Infinities and NaN of rows that are masked for some row of the other side must not reach it, and in a matrix product they do
+// (0 x NaN).  They are rare, and show: the walk over the tiles ends with a NaN among the workgroup's sums.  It is then done once more, now with
+// zeros in the place of such values in the tiles that are not seen whole by the whole workgroup, and a look at each row of those
+// tiles adds what the pairs that are seen would have received.
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t u) { return ((u & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ __forceinline__ bool nonfinite8(uint4 u) {
     return (nonfinite2(u.x) | nonfinite2(u.y) | nonfinite2(u.z) | nonfinite2(u.w)) != 0;
 }
 __device__ __forceinline__ uint32_t finite2(uint32_t u) { return u & ~((nonfinite2(u) >> 15) * 0xffffu); }
 template <int HD>
-__device__ __forceinline__ void tile_clean(Tile<HD>& t, int& found, int tid) {
+__device__ __forceinline__ void tile_clean(Tile<HD>& t, int tid) {
     const int lane = tid & 63, w = tid >> 6;
 #pragma unroll
     for (int q = 0; q < HD / 32; ++q) {
@@ -174,8 +176,16 @@ __device__ __forceinline__ void tile_clean(Tile<HD>& t, int& found, int tid) {
         const uint4 u = *at;
         if (!nonfinite8(u)) continue;
         *at = make_uint4(finite2(u.x), finite2(u.y), finite2(u.z), finite2(u.w));
-        found = 1;
     }
+}
+template <int N>
+__device__ __forceinline__ bool any_nonfinite(const f32x16 (&x)[N]) {
+    float s = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s = fmaf(x[n][i], 0.f, s);
+    return s != s;
 }
 // whether a row of HD values (at `row`, in memory) has an infinity or a NaN among them; the same for the whole wave
 template <int HD>
@@ -214,48 +224,34 @@ template <int HD>
 struct FwdShared {
     Tile<HD> k[2], v[2];
     Ends ends[4];
-    int found;       // infinities or NaN in a tile that is not seen whole
 };
-template <int HD, int OWN, int WPE, bool CAP, bool BIAS>
+template <int HD, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
                                                       const bf16_t* __restrict__ V, const float* __restrict__ slopes,
                                                       bf16_t* __restrict__ O, float* __restrict__ L, float4* __restrict__ sums,
                                                       float2* __restrict__ stat, Order order, Rows rows, Score sc) {
-    constexpr int NI = OWN / 32, NK = HD / 16, NV = HD / 32, WG = 4 * OWN;
-    static_assert(NI == 1, "a wave's 32 queries (the parts' layout)");
-    constexpr bool RAW = !CAP && !BIAS;     // the products themselves are compared, and scaled with the subtraction
+    constexpr int NK = HD / 16, NV = HD / 32;
     __shared__ FwdShared<HD> sm;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, h = lane >> 5;
     Place at;
     if (!place<false>(order, at)) return;
     const int T = rows.Tk;          // rows of the streamed side, for the tile loads
-    const int i0 = (order.nblk - 1 - at.rank) * WG, q0 = i0 + OWN * w;
+    const int i0 = (order.nblk - 1 - at.rank) * BLOCK, q0 = i0 + 32 * w, qi = q0 + r32;
     const int b = at.kv / order.Hk, head = b * order.H + (at.kv - b * order.Hk) * order.G + at.g;
     const bf16_t* Kh = K + (size_t)at.kv * T * HD;
     const bf16_t* Vh = V + (size_t)at.kv * T * HD;
     const size_t row0 = (size_t)head * rows.T;
 
-    bf16x8 qf[NI][NK];
-    f32x16 acc[NV][NI];
-    float lsum[NI], m[NI];
-    Range rg[NI];
-    Ends mine{T, 0, 0, T};
+    bf16x8 qf[NK];
+    f32x16 acc[NV];
+    float lsum, m;
 #pragma unroll
-    for (int ib = 0; ib < NI; ++ib) {
-        const int i = min(q0 + 32 * ib + r32, rows.T - 1);
-        lsum[ib] = 0.f;
-        m[ib] = NEG_INF;
-        rg[ib] = row_range(rows, b, i);
-        mine = join(mine, wave_ends<false>(rg[ib]));
-#pragma unroll
-        for (int ks = 0; ks < NK; ++ks) qf[ib][ks] = row_frag_global<HD>(Q, row0 + i, ks, h);
-#pragma unroll
-        for (int vb = 0; vb < NV; ++vb) acc[vb][ib] = splat16(0.f);
-    }
+    for (int ks = 0; ks < NK; ++ks) qf[ks] = row_frag_global<HD>(Q, row0 + min(qi, rows.T - 1), ks, h);
+    const Range rg = row_range(rows, b, min(qi, rows.T - 1));
+    const Ends mine = wave_ends<false>(rg);
     const float slope = BIAS ? slopes[head - b * order.H] * LOG2E : 0.f;
 
     if (lane == 0) sm.ends[w] = mine;
-    if (tid == 0) sm.found = 0;
     __syncthreads();
     Ends all = join(join(sm.ends[0], sm.ends[1]), join(sm.ends[2], sm.ends[3]));
     int t_lo = __builtin_amdgcn_readfirstlane(all.lo_min) / AT, t_hi = (__builtin_amdgcn_readfirstlane(all.hi_max) + AT - 1) / AT;
@@ -265,129 +261,126 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
         t_hi = first + (int)((long long)n * (at.part + 1) / order.parts);
     }
 
+    // In log 2 units the score is s = factor x + offset, with x what is compared and masked: the product itself, or minus the r of a
+    // capped one; with a bias the score.
+    const float factor = BIAS ? 1.f : CAP ? 2.f * sc.capl : sc.sl, offset = CAP && !BIAS ? sc.capl : 0.f;
     const Reads<HD> rd(lane);
     auto tile = [&](int buf, int key0, bool masked) {
         const uint32_t kt = lds_address(sm.k[0].at) + buf * Tile<HD>::BYTES, vt = kt + 2 * Tile<HD>::BYTES;
-        f32x16 c[2][NI];        // S^T: key 32 kb + 8 k + 4 h + r, query 32 ib + r32
+        f32x16 c[2];        // S^T: key 32 kb + 8 k + 4 h + r, query r32
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
+            c[kb] = splat16(0.f);
 #pragma unroll
-            for (int ib = 0; ib < NI; ++ib) c[kb][ib] = splat16(0.f);
-#pragma unroll
-            for (int ks = 0; ks < NK; ++ks) {
-                const bf16x8 kf = row_op<HD>(kt, rd, kb, ks);
-#pragma unroll
-                for (int ib = 0; ib < NI; ++ib) c[kb][ib] = mfma32(kf, qf[ib][ks], c[kb][ib]);
-            }
+            for (int ks = 0; ks < NK; ++ks) c[kb] = mfma32(row_op<HD>(kt, rd, kb, ks), qf[ks], c[kb]);
         }
-        float mm[NI];
-#pragma unroll
-        for (int ib = 0; ib < NI; ++ib) {
-            const float far = BIAS ? (float)(q0 + 32 * ib + r32 + rows.off - key0 - 4 * h) : 0.f;
-            if (!RAW)
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float x = c[kb][ib][i];
-                        if (CAP) x = fmaf(-2.f * sc.capl, cap_r(x, sc), sc.capl);
-                        else x *= sc.sl;
-                        if (BIAS) x = fmaf(-slope, fabsf(far - (float)(32 * kb + 8 * (i >> 2) + (i & 3))), x);
-                        c[kb][ib][i] = x;
-                    }
-            if (masked) {
-                const int key = key0 + 4 * h - rg[ib].lo, n = max(rg[ib].hi - rg[ib].lo, 0);
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if ((unsigned)(key + 32 * kb + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) c[kb][ib][i] = NEG_INF;
-            }
-            float top[2] = {NEG_INF, NEG_INF};
+        if (CAP || BIAS) {
+            const float far = BIAS ? (float)(qi + rows.off - key0 - 4 * h) : 0.f;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) top[kb] = fmaxf(top[kb], c[kb][ib][i]);
-            float lo, hi;
-            halves(fmaxf(top[0], top[1]), lo, hi);
-            const float t = RAW ? fmaxf(lo, hi) * sc.sl : fmaxf(lo, hi);
-            if (__any(t > m[ib] + 8.f)) {
-                const float to = fmaxf(t, m[ib]);
-                const float f = to == NEG_INF ? 1.f : __builtin_amdgcn_exp2f(m[ib] - to);
-                m[ib] = to;
-                lsum[ib] *= f;
-#pragma unroll
-                for (int vb = 0; vb < NV; ++vb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[vb][ib][i] *= f;
-            }
-            mm[ib] = m[ib] == NEG_INF ? 0.f : m[ib];
+                for (int i = 0; i < 16; ++i) {
+                    float x = c[kb][i];
+                    if (CAP) {
+                        x = -cap_r(x, sc);
+                        if (BIAS) x = fmaf(2.f * sc.capl, x, sc.capl);
+                    } else {
+                        x *= sc.sl;
+                    }
+                    if (BIAS) x = fmaf(-slope, fabsf(far - (float)(32 * kb + 8 * (i >> 2) + (i & 3))), x);
+                    c[kb][i] = x;
+                }
         }
+        if (masked) {
+            const int key = key0 + 4 * h - rg.lo, n = max(rg.hi - rg.lo, 0);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if ((unsigned)(key + 32 * kb + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) c[kb][i] = NEG_INF;
+        }
+        float top[2] = {NEG_INF, NEG_INF};
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top[kb] = fmaxf(top[kb], c[kb][i]);
+        float lo, hi;
+        halves(fmaxf(top[0], top[1]), lo, hi);
+        const float t = fmaf(fmaxf(lo, hi), factor, offset);
+        if (__any(t > m + 8.f)) {
+            const float to = fmaxf(t, m);
+            const float f = to == NEG_INF ? 1.f : __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            lsum *= f;
+#pragma unroll
+            for (int vb = 0; vb < NV; ++vb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[vb][i] *= f;
+        }
+        const float by = offset - (m == NEG_INF ? 0.f : m);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            Frag pf[NI][2];
+            Frag pf[2];
 #pragma unroll
-            for (int ib = 0; ib < NI; ++ib) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x = c[kb][ib][i], p = __builtin_amdgcn_exp2f(RAW ? fmaf(x, sc.sl, -mm[ib]) : x - mm[ib]);
-                    lsum[ib] += p;      // (unrounded: L is a result)
-                    pf[ib][i >> 3].v[i & 7] = (__bf16)p;
-                }
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(BIAS ? c[kb][i] + by : fmaf(c[kb][i], factor, by));
+                lsum += p;      // (unrounded: L is a result)
+                pf[i >> 3].v[i & 7] = (__bf16)p;
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int vb = 0; vb < NV; ++vb) {
-                    const bf16x8 vf = col_op<HD>(vt, rd, 2 * kb + j, vb);
-#pragma unroll
-                    for (int ib = 0; ib < NI; ++ib) acc[vb][ib] = mfma32(vf, pf[ib][j].v, acc[vb][ib]);
-                }
+                for (int vb = 0; vb < NV; ++vb) acc[vb] = mfma32(col_op<HD>(vt, rd, 2 * kb + j, vb), pf[j].v, acc[vb]);
         }
     };
 
-    if (t_lo < t_hi) {
-        tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
-        tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
-    }
-    dma_arrived<0>();
-    __syncthreads();
-    for (int t = t_lo; t < t_hi; ++t) {
-        const int buf = (t - t_lo) & 1, key0 = t * AT;
-        if (t + 1 < t_hi) {
-            tile_load(sm.k[buf ^ 1], Kh, key0 + AT, T, lane, w);
-            tile_load(sm.v[buf ^ 1], Vh, key0 + AT, T, lane, w);
+    bool careful = false;
+    for (;;) {
+#pragma unroll
+        for (int vb = 0; vb < NV; ++vb) acc[vb] = splat16(0.f);
+        lsum = 0.f;
+        m = NEG_INF;
+        if (t_lo < t_hi) {
+            tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
+            tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
         }
-        if (!all.all(key0, AT)) {
-            tile_clean(sm.v[buf], sm.found, tid);
-            lds_barrier();
-        }
-        if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
         dma_arrived<0>();
         __syncthreads();
+        for (int t = t_lo; t < t_hi; ++t) {
+            const int buf = (t - t_lo) & 1, key0 = t * AT;
+            if (t + 1 < t_hi) {
+                tile_load(sm.k[buf ^ 1], Kh, key0 + AT, T, lane, w);
+                tile_load(sm.v[buf ^ 1], Vh, key0 + AT, T, lane, w);
+            }
+            if (careful && !all.all(key0, AT)) {
+                tile_clean(sm.v[buf], tid);
+                lds_barrier();
+            }
+            if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
+            dma_arrived<0>();
+            __syncthreads();
+        }
+        if (careful || !__syncthreads_or(any_nonfinite(acc))) break;
+        careful = true;
     }
 
-    if (sm.found != 0) {     // the values that entered as zeros
+    if (careful) {     // the values that entered as zeros
         for (int t = t_lo; t < t_hi; ++t) {
             if (all.all(t * AT, AT) || mine.none(t * AT, AT)) continue;
             for (int key = t * AT; key < min(t * AT + AT, T); ++key) {
-                bool any = false;
-#pragma unroll
-                for (int ib = 0; ib < NI; ++ib) any |= sees(key, rg[ib]);
                 const bf16_t* v = Vh + (size_t)key * HD;
-                if (!__any(any) || !row_nonfinite<HD>(v, lane)) continue;
+                if (!__any(sees(key, rg)) || !row_nonfinite<HD>(v, lane)) continue;
 #pragma unroll
-                for (int ib = 0; ib < NI; ++ib)
+                for (int vb = 0; vb < NV; ++vb)
 #pragma unroll
-                    for (int vb = 0; vb < NV; ++vb)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const uint32_t u = v[32 * vb + 8 * (i >> 2) + 4 * h + (i & 3)];
-                            if (nonfinite2(u) != 0 && sees(key, rg[ib])) acc[vb][ib][i] += __uint_as_float(u << 16);
-                        }
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t u = v[32 * vb + 8 * (i >> 2) + 4 * h + (i & 3)];
+                        if (nonfinite2(u) != 0 && sees(key, rg)) acc[vb][i] += __uint_as_float(u << 16);
+                    }
             }
         }
     }
+    const float z = xor32_sum(lsum);
     if (order.parts > 1) {
         const size_t slot = (((size_t)at.part * order.BHk * order.G + (size_t)at.kv * order.G + at.g) * order.nblk + at.rank) * 4 + w;
         float4* to = sums + slot * (4 * NV * 64) + lane;
@@ -395,21 +388,16 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
         for (int vb = 0; vb < NV; ++vb)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-                to[(4 * vb + k) * 64] = make_float4(acc[vb][0][4 * k], acc[vb][0][4 * k + 1], acc[vb][0][4 * k + 2], acc[vb][0][4 * k + 3]);
-        const float z = xor32_sum(lsum[0]);
-        if (h == 0) stat[slot * 32 + r32] = make_float2(m[0], z);
+                to[(4 * vb + k) * 64] = make_float4(acc[vb][4 * k], acc[vb][4 * k + 1], acc[vb][4 * k + 2], acc[vb][4 * k + 3]);
+        if (h == 0) stat[slot * 32 + r32] = make_float2(m, z);
         return;
     }
+    const bool in = qi < rows.T;
+    const size_t row = row0 + min(qi, rows.T - 1);
+    const float f = z != 0.f ? 1.f / z : 0.f;
 #pragma unroll
-    for (int ib = 0; ib < NI; ++ib) {
-        const int i = q0 + 32 * ib + r32;
-        const bool in = i < rows.T;
-        const size_t row = row0 + min(i, rows.T - 1);
-        const float z = xor32_sum(lsum[ib]), f = z != 0.f ? 1.f / z : 0.f;
-#pragma unroll
-        for (int vb = 0; vb < NV; ++vb) store_block(O + row * HD + 32 * vb, acc[vb][ib], f, h, in);
-        if (L != nullptr && h == 0 && in) L[row] = z != 0.f ? (m[ib] + __builtin_amdgcn_logf(z)) * LN2 : NEG_INF;
-    }
+    for (int vb = 0; vb < NV; ++vb) store_block(O + row * HD + 32 * vb, acc[vb], f, h, in);
+    if (L != nullptr && h == 0 && in) L[row] = z != 0.f ? (m + __builtin_amdgcn_logf(z)) * LN2 : NEG_INF;
 }
 
 // A block's rows from its parts, 32 values of each (blockIdx.y).  Blocks are numbered as the parts' kernel does, from the last one on.
@@ -485,7 +473,8 @@ __global__ __launch_bounds__(256) void k_exp_prep(const bf16_t* __restrict__ dO,
     if (tid == 0) to.ends[(size_t)b * ntile + t] = make_int4(e.lo_min, e.hi_max, e.lo_max, e.hi_min);
 }
 
-// weight of a pair and, times (dO . v - D), the gradient of its product: p and t from the product c and e = dO . v - D
+// weight of a pair and, times (dO . v - D), the gradient of its product (of a capped one, over 4: the results take
+// that back): p and t from the product c and e = dO . v - D
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ void pair_grad(float c, float e, float l2, float slope, float dist, const Score& sc, float& p, float& t) {
     float r = 0.f, s;
@@ -498,51 +487,41 @@ __device__ __forceinline__ void pair_grad(float c, float e, float l2, float slop
     if (BIAS) s = fmaf(-slope, fabsf(dist), s);
     p = __builtin_amdgcn_exp2f(s);
     t = p * e;
-    if (CAP) t *= 4.f * fmaf(-r, r, r);
+    if (CAP) t *= fmaf(-r, r, r);
 }
 
 // ---- backward: dQ -------------------------------------------------------------------------------------------
 // acc[fb][ib] = dQ^T / scale: features 32 fb + .., query 32 ib + r32.
-template <int HD, int OWN, int WPE, bool CAP, bool BIAS>
+template <int HD, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
                                                      const bf16_t* __restrict__ V, const float* __restrict__ slopes,
                                                      const bf16_t* __restrict__ dO, const float2* __restrict__ stat,
                                                      bf16_t* __restrict__ dQ, Order order, Rows rows, Score sc, float scale) {
-    constexpr int NI = OWN / 32, NK = HD / 16, NF = HD / 32, WG = 4 * OWN;
+    constexpr int NK = HD / 16, NF = HD / 32;
     __shared__ FwdShared<HD> sm;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, h = lane >> 5;
     Place at;
     if (!place<false>(order, at)) return;
     const int T = rows.Tk;
-    const int i0 = (order.nblk - 1 - at.rank) * WG, q0 = i0 + OWN * w;
+    const int i0 = (order.nblk - 1 - at.rank) * BLOCK, q0 = i0 + 32 * w, qi = q0 + r32;
     const int b = at.kv / order.Hk, head = b * order.H + (at.kv - b * order.Hk) * order.G + at.g;
     const bf16_t* Kh = K + (size_t)at.kv * T * HD;
     const bf16_t* Vh = V + (size_t)at.kv * T * HD;
     const size_t row0 = (size_t)head * rows.T;
 
-    bf16x8 qf[NI][NK], gf[NI][NK];
-    f32x16 acc[NF][NI];
-    float2 st[NI];
-    Range rg[NI];
-    Ends mine{T, 0, 0, T};
+    bf16x8 qf[NK], gf[NK];
+    f32x16 acc[NF];
 #pragma unroll
-    for (int ib = 0; ib < NI; ++ib) {
-        const int i = min(q0 + 32 * ib + r32, rows.T - 1);
-        st[ib] = stat[row0 + i];
-        rg[ib] = row_range(rows, b, i);
-        mine = join(mine, wave_ends<false>(rg[ib]));
-#pragma unroll
-        for (int ks = 0; ks < NK; ++ks) {
-            qf[ib][ks] = row_frag_global<HD>(Q, row0 + i, ks, h);
-            gf[ib][ks] = row_frag_global<HD>(dO, row0 + i, ks, h);
-        }
-#pragma unroll
-        for (int fb = 0; fb < NF; ++fb) acc[fb][ib] = splat16(0.f);
+    for (int ks = 0; ks < NK; ++ks) {
+        qf[ks] = row_frag_global<HD>(Q, row0 + min(qi, rows.T - 1), ks, h);
+        gf[ks] = row_frag_global<HD>(dO, row0 + min(qi, rows.T - 1), ks, h);
     }
+    const float2 st = stat[row0 + min(qi, rows.T - 1)];
+    const Range rg = row_range(rows, b, min(qi, rows.T - 1));
+    const Ends mine = wave_ends<false>(rg);
     const float slope = BIAS ? slopes[head - b * order.H] * LOG2E : 0.f;
 
     if (lane == 0) sm.ends[w] = mine;
-    if (tid == 0) sm.found = 0;
     __syncthreads();
     Ends all = join(join(sm.ends[0], sm.ends[1]), join(sm.ends[2], sm.ends[3]));
     const int t_lo = __builtin_amdgcn_readfirstlane(all.lo_min) / AT, t_hi = (__builtin_amdgcn_readfirstlane(all.hi_max) + AT - 1) / AT;
@@ -552,97 +531,79 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
         const uint32_t kt = lds_address(sm.k[0].at) + buf * Tile<HD>::BYTES, vt = kt + 2 * Tile<HD>::BYTES;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            f32x16 c[NI], e[NI];        // S^T and (dO V^T - D)^T: key 32 kb + 8 k + 4 h + r, query 32 ib + r32
-#pragma unroll
-            for (int ib = 0; ib < NI; ++ib) {
-                c[ib] = splat16(0.f);
-                e[ib] = splat16(st[ib].y);
-            }
+            f32x16 c = splat16(0.f), e = splat16(st.y);     // S^T and (dO V^T - D)^T: key 32 kb + 8 k + 4 h + r, query r32
 #pragma unroll
             for (int ks = 0; ks < NK; ++ks) {
-                const bf16x8 kf = row_op<HD>(kt, rd, kb, ks), vf = row_op<HD>(vt, rd, kb, ks);
-#pragma unroll
-                for (int ib = 0; ib < NI; ++ib) {
-                    c[ib] = mfma32(kf, qf[ib][ks], c[ib]);
-                    e[ib] = mfma32(vf, gf[ib][ks], e[ib]);
-                }
+                c = mfma32(row_op<HD>(kt, rd, kb, ks), qf[ks], c);
+                e = mfma32(row_op<HD>(vt, rd, kb, ks), gf[ks], e);
                 if (ks & 1) __builtin_amdgcn_sched_barrier(0);
             }
-            Frag tf[NI][2];
+            const float far = BIAS ? (float)(qi + rows.off - key0 - 32 * kb - 4 * h) : 0.f;
 #pragma unroll
-            for (int ib = 0; ib < NI; ++ib) {
-                const float far = BIAS ? (float)(q0 + 32 * ib + r32 + rows.off - key0 - 32 * kb - 4 * h) : 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = 8 * (i >> 2) + (i & 3);
-                    float p, t;
-                    pair_grad<CAP, BIAS>(c[ib][i], e[ib][i], st[ib].x, slope, far - (float)key, sc, p, t);
-                    e[ib][i] = t;
-                }
-                if (masked) {
-                    const int key = key0 + 32 * kb + 4 * h - rg[ib].lo, n = max(rg[ib].hi - rg[ib].lo, 0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if ((unsigned)(key + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) e[ib][i] = 0.f;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) tf[ib][i >> 3].v[i & 7] = (__bf16)e[ib][i];
+            for (int i = 0; i < 16; ++i) {
+                float p, t;
+                pair_grad<CAP, BIAS>(c[i], e[i], st.x, slope, far - (float)(8 * (i >> 2) + (i & 3)), sc, p, t);
+                e[i] = t;
             }
+            if (masked) {
+                const int key = key0 + 32 * kb + 4 * h - rg.lo, n = max(rg.hi - rg.lo, 0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if ((unsigned)(key + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) e[i] = 0.f;
+            }
+            Frag tf[2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) tf[i >> 3].v[i & 7] = (__bf16)e[i];
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int fb = 0; fb < NF; ++fb) {
-                    const bf16x8 kc = col_op<HD>(kt, rd, 2 * kb + j, fb);   // K^T
-#pragma unroll
-                    for (int ib = 0; ib < NI; ++ib) acc[fb][ib] = mfma32(kc, tf[ib][j].v, acc[fb][ib]);
-                }
+                for (int fb = 0; fb < NF; ++fb) acc[fb] = mfma32(col_op<HD>(kt, rd, 2 * kb + j, fb), tf[j].v, acc[fb]);     // K^T
         }
     };
 
-    if (t_lo < t_hi) {
-        tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
-        tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
-    }
-    dma_arrived<0>();
-    __syncthreads();
-    for (int t = t_lo; t < t_hi; ++t) {
-        const int buf = (t - t_lo) & 1, key0 = t * AT;
-        if (t + 1 < t_hi) {
-            tile_load(sm.k[buf ^ 1], Kh, key0 + AT, T, lane, w);
-            tile_load(sm.v[buf ^ 1], Vh, key0 + AT, T, lane, w);
+    bool careful = false;
+    for (;;) {
+#pragma unroll
+        for (int fb = 0; fb < NF; ++fb) acc[fb] = splat16(0.f);
+        if (t_lo < t_hi) {
+            tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
+            tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
         }
-        if (!all.all(key0, AT)) {
-            tile_clean(sm.k[buf], sm.found, tid);
-            lds_barrier();
-        }
-        if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
         dma_arrived<0>();
         __syncthreads();
+        for (int t = t_lo; t < t_hi; ++t) {
+            const int buf = (t - t_lo) & 1, key0 = t * AT;
+            if (t + 1 < t_hi) {
+                tile_load(sm.k[buf ^ 1], Kh, key0 + AT, T, lane, w);
+                tile_load(sm.v[buf ^ 1], Vh, key0 + AT, T, lane, w);
+            }
+            if (careful && !all.all(key0, AT)) {
+                tile_clean(sm.k[buf], tid);
+                lds_barrier();
+            }
+            if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
+            dma_arrived<0>();
+            __syncthreads();
+        }
+        if (careful || !__syncthreads_or(any_nonfinite(acc))) break;
+        careful = true;
     }
 
-    if (sm.found != 0) {     // nothing is left of the rows that see a key that is no finite vector
+    if (careful) {     // nothing is left of the rows that see a key that is no finite vector
         for (int t = t_lo; t < t_hi; ++t) {
             if (all.all(t * AT, AT) || mine.none(t * AT, AT)) continue;
             for (int key = t * AT; key < min(t * AT + AT, T); ++key) {
-                bool any = false;
+                if (!__any(sees(key, rg)) || !row_nonfinite<HD>(Kh + (size_t)key * HD, lane)) continue;
+                if (sees(key, rg))
 #pragma unroll
-                for (int ib = 0; ib < NI; ++ib) any |= sees(key, rg[ib]);
-                if (!__any(any) || !row_nonfinite<HD>(Kh + (size_t)key * HD, lane)) continue;
-#pragma unroll
-                for (int ib = 0; ib < NI; ++ib)
-                    if (sees(key, rg[ib]))
-#pragma unroll
-                        for (int fb = 0; fb < NF; ++fb) acc[fb][ib] = splat16(__builtin_nanf(""));
+                    for (int fb = 0; fb < NF; ++fb) acc[fb] = splat16(__builtin_nanf(""));
             }
         }
     }
+    const float f = scale * (CAP ? 4.f : 1.f);
+    const size_t row = row0 + min(qi, rows.T - 1);
 #pragma unroll
-    for (int ib = 0; ib < NI; ++ib) {
-        const int i = q0 + 32 * ib + r32;
-        const size_t row = row0 + min(i, rows.T - 1);
-#pragma unroll
-        for (int fb = 0; fb < NF; ++fb) store_block(dQ + row * HD + 32 * fb, acc[fb][ib], scale, h, i < rows.T);
-    }
+    for (int fb = 0; fb < NF; ++fb) store_block(dQ + row * HD + 32 * fb, acc[fb], f, h, qi < rows.T);
 }
 
 // ---- backward: dK, dV -----------------------------------------------------------------------------------------
@@ -654,8 +615,7 @@ template <int HD>
 struct BwdShared {
     Tile<HD> q[2], g[2];
     float l2[2][AT], d[2][AT];
-    int lo[2][AT], hi[2][AT];
-    int found;
+    int lo[2][AT], n[2][AT];        // keys lo .. lo + n - 1
 };
 template <int HD, int OWN, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
@@ -685,14 +645,12 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
             kf[kb][ks] = row_frag_global<HD>(K, row, ks, h);
             vf[kb][ks] = row_frag_global<HD>(V, row, ks, h);
         }
-#pragma unroll
-        for (int fb = 0; fb < NF; ++fb) {
-            dk[fb][kb] = splat16(0.f);
-            dv[fb][kb] = splat16(0.f);
-        }
     }
-    if (tid == 0) sm.found = 0;
-    __syncthreads();
+    // (from the scalar cache: a vector load would make the wave wait for the tile on its way)
+    auto head_slope = [&](int g) {
+        typedef __attribute__((address_space(4))) const float constant_float;
+        return ((constant_float*)(uintptr_t)slopes)[head0 + g - b * order.H] * LOG2E;
+    };
 
     const Reads<HD> rd(lane);
     auto tile = [&](int buf, int q0, float slope, bool masked) {
@@ -733,9 +691,12 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
                 }
                 if (masked) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int row = 32 * qb + 4 * h + 8 * (i >> 2) + (i & 3);
-                        if (!sees(key, {sm.lo[buf][row], sm.hi[buf][row]})) c[kb][i] = e[kb][i] = 0.f;
+                    for (int k = 0; k < 4; ++k) {
+                        const int4 lo = *(const int4*)&sm.lo[buf][32 * qb + 8 * k + 4 * h], n = *(const int4*)&sm.n[buf][32 * qb + 8 * k + 4 * h];
+                        if ((unsigned)(key - lo.x) >= (unsigned)n.x) c[kb][4 * k] = e[kb][4 * k] = 0.f;
+                        if ((unsigned)(key - lo.y) >= (unsigned)n.y) c[kb][4 * k + 1] = e[kb][4 * k + 1] = 0.f;
+                        if ((unsigned)(key - lo.z) >= (unsigned)n.z) c[kb][4 * k + 2] = e[kb][4 * k + 2] = 0.f;
+                        if ((unsigned)(key - lo.w) >= (unsigned)n.w) c[kb][4 * k + 3] = e[kb][4 * k + 3] = 0.f;
                     }
                 }
 #pragma unroll
@@ -759,89 +720,109 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
         }
     };
 
-    // the tiles of rows that see a key of the block, for one head after the other, 64 tiles at a time
-    int base = -64, g = order.G, turn = 0;
-    uint64_t seen = 0, left = 0;
-    auto advance = [&]() -> int {
+    // the tiles of rows that see a key of the block, for one head after the other, 64 tiles at a time; their ends are in the lanes
+    struct Item {
+        int t, g;
+        Ends e;
+    };
+    int base, g, turn;
+    uint64_t seen, left;
+    int4 le = make_int4(0, 0, 0, 0);
+    auto restart = [&]() {
+        base = -64;
+        g = order.G;
+        turn = 0;
+        seen = left = 0;
+    };
+    auto advance = [&](Item& it) -> bool {
         for (;;) {
             while (left == 0) {
                 if (++g < order.G) {
                     left = seen;
                 } else {
                     base += 64;
-                    if (base >= ntile) return -1;
-                    const int t = base + lane;
-                    const int4 e = ends[min(t, ntile - 1)];
-                    seen = left = __ballot(t < ntile && !Ends{e.x, e.y, e.z, e.w}.none(j0, WG));
+                    if (base >= ntile) return false;
+                    le = ends[min(base + lane, ntile - 1)];
+                    seen = left = __ballot(base + lane < ntile && !Ends{le.x, le.y, le.z, le.w}.none(j0, WG));
                     g = seen != 0 ? 0 : order.G;
                 }
             }
-            const int t = base + __builtin_ctzll(left);
+            const int n = __builtin_ctzll(left);
             left &= left - 1;
             const bool mine = turn == at.part;
             turn = turn + 1 == order.parts ? 0 : turn + 1;
-            if (mine) return t;
+            if (mine) {
+                it = {base + n, g,
+                      {__builtin_amdgcn_readlane(le.x, n), __builtin_amdgcn_readlane(le.y, n), __builtin_amdgcn_readlane(le.z, n),
+                       __builtin_amdgcn_readlane(le.w, n)}};
+                return true;
+            }
         }
     };
     float2 str = make_float2(0.f, 0.f);
     int2 rgr = make_int2(0, 0);
-    auto load = [&](int t, int head, int buf) {
-        const size_t base_row = (size_t)head * T;
+    auto load = [&](const Item& it, int buf) {
+        const size_t head = (size_t)(head0 + it.g) * T;
         if (tid < AT) {
-            const int i = min(t * AT + tid, T - 1);
-            str = from.stat[base_row + i];
-            rgr = t * AT + tid < T ? range[i] : make_int2(rows.Tk, 0);
+            const int i = min(it.t * AT + tid, T - 1);
+            str = from.stat[head + i];
+            rgr = it.t * AT + tid < T ? range[i] : make_int2(rows.Tk, 0);
         }
-        tile_load(sm.q[buf], Q + base_row * HD, t * AT, T, lane, w);
-        tile_load(sm.g[buf], dO + base_row * HD, t * AT, T, lane, w);
+        tile_load(sm.q[buf], Q + head * HD, it.t * AT, T, lane, w);
+        tile_load(sm.g[buf], dO + head * HD, it.t * AT, T, lane, w);
     };
     auto store = [&](int buf) {
         if (tid < AT) {
             sm.l2[buf][tid] = str.x;
             sm.d[buf][tid] = str.y;
             sm.lo[buf][tid] = rgr.x;
-            sm.hi[buf][tid] = rgr.y;
+            sm.n[buf][tid] = max(rgr.y - rgr.x, 0);
         }
     };
-    auto ends_of = [&](int t) {
-        const int4 e = ends[t];
-        return Ends{__builtin_amdgcn_readfirstlane(e.x), __builtin_amdgcn_readfirstlane(e.y), __builtin_amdgcn_readfirstlane(e.z),
-                    __builtin_amdgcn_readfirstlane(e.w)};
-    };
-    int t = advance(), gt = g, buf = 0;
-    Ends e{0, 0, 0, 0};
-    if (t >= 0) {
-        e = ends_of(t);
-        load(t, head0 + gt, 0);
-        store(0);
-    }
-    dma_arrived<0>();
-    __syncthreads();
-    while (t >= 0) {
-        const int tn = advance(), gn = g;
-        Ends en{0, 0, 0, 0};
-        if (tn >= 0) {
-            en = ends_of(tn);
-            load(tn, head0 + gn, buf ^ 1);
+    bool careful = false;
+    for (;;) {
+#pragma unroll
+        for (int kb = 0; kb < NJ; ++kb)
+#pragma unroll
+            for (int fb = 0; fb < NF; ++fb) {
+                dk[fb][kb] = splat16(0.f);
+                dv[fb][kb] = splat16(0.f);
+            }
+        restart();
+        Item now{0, 0, {0, 0, 0, 0}}, next = now;
+        bool more = advance(now);
+        if (more) {
+            load(now, 0);
+            store(0);
         }
-        if (!e.all(j0, WG)) {
-            tile_clean(sm.q[buf], sm.found, tid);
-            tile_clean(sm.g[buf], sm.found, tid);
-            lds_barrier();
-        }
-        if (!e.none(k0, OWN)) tile(buf, t * AT, BIAS ? slopes[head0 + gt - b * order.H] * LOG2E : 0.f, !e.all(k0, OWN));
-        if (tn >= 0) store(buf ^ 1);
-        buf ^= 1;
-        t = tn;
-        gt = gn;
-        e = en;
         dma_arrived<0>();
         __syncthreads();
+        for (int buf = 0; more; buf ^= 1) {
+            const bool another = advance(next);
+            if (another) load(next, buf ^ 1);
+            if (careful && !now.e.all(j0, WG)) {
+                tile_clean(sm.q[buf], tid);
+                tile_clean(sm.g[buf], tid);
+                lds_barrier();
+            }
+            if (!now.e.none(k0, OWN)) tile(buf, now.t * AT, BIAS ? head_slope(now.g) : 0.f, !now.e.all(k0, OWN));
+            if (another) store(buf ^ 1);
+            now = next;
+            more = another;
+            dma_arrived<0>();
+            __syncthreads();
+        }
+        bool bad = false;
+#pragma unroll
+        for (int fb = 0; fb < NF; ++fb) bad |= any_nonfinite(dk[fb]) || any_nonfinite(dv[fb]);
+        if (careful || !__syncthreads_or(bad)) break;
+        careful = true;
     }
 
-    if (sm.found != 0) {     // nothing is left of the keys that a row sees whose query or gradient is no finite vector
+    if (careful) {     // nothing is left of the keys that a row sees whose query or gradient is no finite vector
         for (int t = 0; t < ntile; ++t) {
-            const Ends e = ends_of(t);
+            const int4 x = ends[t];
+            const Ends e{x.x, x.y, x.z, x.w};
             if (e.all(j0, WG) || e.none(k0, OWN)) continue;
             for (int i = t * AT; i < min(t * AT + AT, T); ++i) {
                 const Range rg{range[i].x, range[i].y};
@@ -850,8 +831,8 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
                 for (int kb = 0; kb < NJ; ++kb) any |= sees(k0 + 32 * kb + r32, rg);
                 if (!__any(any)) continue;
                 bool bad = false;
-                for (int g = 0; g < order.G; ++g) {
-                    const size_t row = ((size_t)(head0 + g) * T + i) * HD;
+                for (int hd = 0; hd < order.G; ++hd) {
+                    const size_t row = ((size_t)(head0 + hd) * T + i) * HD;
                     bad |= row_nonfinite<HD>(Q + row, lane) || row_nonfinite<HD>(dO + row, lane);
                 }
                 if (!bad) continue;
@@ -881,7 +862,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dkdv(const bf16_t* __restrict_
         const size_t row = key_row0 + min(key, rows.Tk - 1);
 #pragma unroll
         for (int fb = 0; fb < NF; ++fb) {
-            store_block(dK + row * HD + 32 * fb, dk[fb][kb], scale, h, key < rows.Tk);
+            store_block(dK + row * HD + 32 * fb, dk[fb][kb], scale * (CAP ? 4.f : 1.f), h, key < rows.Tk);
             store_block(dV + row * HD + 32 * fb, dv[fb][kb], 1.f, h, key < rows.Tk);
         }
     }
@@ -932,7 +913,7 @@ long long blocks_of(const Order& o, bool per_key_head) {
 
 template <int HD>
 struct Shape {
-    static constexpr int FWD_OWN = 32, FWD_WPE = 2, DQ_WPE = 2, DKDV_WPE = HD == 128 ? 1 : 2;
+    static constexpr int DKDV_WPE = HD == 128 ? 1 : 2;
 };
 
 // Workgroups per block of 128 queries: until there are two per CU, as long as each has 8 tiles or more of those that the block may have
@@ -955,14 +936,13 @@ FwdParts fwd_part_bytes(const pa_exp_problem& pr, int parts) {
 template <int HD, bool CAP, bool BIAS>
 pa_status fwd_t(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, const bf16_t* V, const ExpMask& mk, const Rows& rows, bf16_t* O,
                 float* L, char* ws, hipStream_t s) {
-    constexpr int OWN = Shape<HD>::FWD_OWN;
-    Order o = order_of(pr, 4 * OWN, pr.T);
+    Order o = order_of(pr, BLOCK, pr.T);
     o.parts = fwd_parts(pr, rows.hi != nullptr);
     float4* sums = (float4*)ws;
     float2* stat = (float2*)(ws + fwd_part_bytes(pr, o.parts).sums);
     {
         LaunchScope ls("exp_fwd", s);
-        hipLaunchKernelGGL((k_exp_fwd<HD, OWN, Shape<HD>::FWD_WPE, CAP, BIAS>), dim3((unsigned)blocks_of(o, false)), dim3(256), 0, s, Q, K, V,
+        hipLaunchKernelGGL((k_exp_fwd<HD, 2, CAP, BIAS>), dim3((unsigned)blocks_of(o, false)), dim3(256), 0, s, Q, K, V,
                            mk.slopes, O, L, sums, stat, o, rows, score_of(pr));
         if (!launch_ok()) return PA_ERR_HIP;
     }
@@ -1013,12 +993,12 @@ pa_status bwd_t(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, cons
     if (ok.parts > 1) {
         LaunchScope ls("exp_bwd_join", s);
         hipLaunchKernelGGL((k_exp_dkdv_join<HD>), dim3((unsigned)(ok.BHk * ok.nblk), HD / 16), dim3(256), 0, s, sums, dK, dV, ok.BHk * ok.nblk,
-                           ok.nblk, ok.parts, pr.Tk, pr.scale);
+                           ok.nblk, ok.parts, pr.Tk, pr.scale * (CAP ? 4.f : 1.f));
         if (!launch_ok()) return PA_ERR_HIP;
     }
     const Order o = order_of(pr, 128, pr.T);
     LaunchScope ls("exp_bwd_dq", s);
-    hipLaunchKernelGGL((k_exp_dq<HD, 32, Shape<HD>::DQ_WPE, CAP, BIAS>), dim3((unsigned)blocks_of(o, false)), dim3(256), 0, s, Q, K, V,
+    hipLaunchKernelGGL((k_exp_dq<HD, 2, CAP, BIAS>), dim3((unsigned)blocks_of(o, false)), dim3(256), 0, s, Q, K, V,
                        mk.slopes, dO, sc.stat, dQ, o, rows, score_of(pr), pr.scale);
     return launch_ok() ? PA_OK : PA_ERR_HIP;
 }
