@@ -98,7 +98,7 @@ struct Tile {
     static constexpr int NROW = HD == 32 ? 2 : 4, NCOL = HD == 128 ? 4 : 2;
     uint4 at[BYTES / 16];
     static __device__ __forceinline__ int turn(int row) {
-        return HD == 128 ? (row & 3) << 2 : HD == 64 ? (row >> 1 & 3) << 1 : (row >> 2 & 1) << 1 | (row >> 3 & 1);
+        return HD == 128 ? (row & 3) << 2 : HD == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 1) << 1 : (row >> 2 & 1) << 1 | (row >> 3 & 1);
     }
     // byte of piece `piece` of a row
     static __device__ __forceinline__ uint32_t place(int row, int piece) {
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
     // capped one; with a bias the score.
     const float factor = BIAS ? 1.f : CAP ? 2.f * sc.capl : sc.sl, offset = CAP && !BIAS ? sc.capl : 0.f;
     const Reads<HD> rd(lane);
-    auto tile = [&](int buf, int key0, bool masked) {
+    auto tile = [&](int buf, int key0) {
         const uint32_t kt = lds_address(sm.k[0].at) + buf * Tile<HD>::BYTES, vt = kt + 2 * Tile<HD>::BYTES;
         f32x16 c[2];        // S^T: key 32 kb + 8 k + 4 h + r, query r32
 #pragma unroll
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
                     c[kb][i] = x;
                 }
         }
-        if (masked) {
+        if (!mine.all(key0, AT)) {      // (both ends at once: in two branches the instances lose a wave per SIMD, and 6 % with it)
             const int key = key0 + 4 * h - rg.lo, n = max(rg.hi - rg.lo, 0);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
                 tile_clean(sm.v[buf], tid);
                 lds_barrier();
             }
-            if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
+            if (!mine.none(key0, AT)) tile(buf, key0);
             dma_arrived<0>();
             __syncthreads();
         }
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
     const int t_lo = __builtin_amdgcn_readfirstlane(all.lo_min) / AT, t_hi = (__builtin_amdgcn_readfirstlane(all.hi_max) + AT - 1) / AT;
 
     const Reads<HD> rd(lane);
-    auto tile = [&](int buf, int key0, bool masked) {
+    auto tile = [&](int buf, int key0) {
         const uint32_t kt = lds_address(sm.k[0].at) + buf * Tile<HD>::BYTES, vt = kt + 2 * Tile<HD>::BYTES;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -545,11 +545,17 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
                 pair_grad<CAP, BIAS>(c[i], e[i], st.x, slope, far - (float)(8 * (i >> 2) + (i & 3)), sc, p, t);
                 e[i] = t;
             }
-            if (masked) {
-                const int key = key0 + 32 * kb + 4 * h - rg.lo, n = max(rg.hi - rg.lo, 0);
+            if (mine.lo_max > key0) {
+                const int lo = rg.lo - key0 - 32 * kb - 4 * h;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if ((unsigned)(key + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) e[i] = 0.f;
+                    if (8 * (i >> 2) + (i & 3) < lo) e[i] = 0.f;
+            }
+            if (mine.hi_min < key0 + AT) {
+                const int hi = rg.hi - key0 - 32 * kb - 4 * h;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (8 * (i >> 2) + (i & 3) >= hi) e[i] = 0.f;
             }
             Frag tf[2];
 #pragma unroll
@@ -581,7 +587,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
                 tile_clean(sm.k[buf], tid);
                 lds_barrier();
             }
-            if (!mine.none(key0, AT)) tile(buf, key0, !mine.all(key0, AT));
+            if (!mine.none(key0, AT)) tile(buf, key0);
             dma_arrived<0>();
             __syncthreads();
         }
