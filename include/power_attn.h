@@ -227,7 +227,7 @@ typedef struct {
     int   B, H, Hk;     /* batch, query heads, key heads (H a multiple of Hk) */
     int   T, Tk, d;     /* queries, keys, head size */
     float scale;        /* > 0 */
-    float cap;          /* > 0: scores are capped by cap tanh(x / cap); 0: they are not */
+    float cap;          /* > 0: scores are capped by cap tanh(x / cap), off by up to 2e-7 cap; 0: they are not.  Up to 1e4 */
     int   window;       /* > 0: only keys behind pos_i - window; 0: no window */
     int   dtype;        /* pa_dtype */
 } pa_exp_problem;

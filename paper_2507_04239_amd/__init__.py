@@ -3,12 +3,23 @@
 ``power_attn_fwd`` / ``power_attn_bwd`` marshal torch device tensors into the C-ABI
 library built from ``csrc/``; every step of the computation runs in its HIP kernels.
 The library is loaded on first use and a missing library is an error, never a fallback.
+
+``power_attn_exp_fwd`` / ``power_attn_exp_bwd`` are exponential (softmax) attention with capped scores, distance bias, document, prefix
+and window masks; ``make_cache`` and ``power_attn_cache_*`` the paged cache (bf16 or 4 bits) that it decodes from.
 """
 from .binding import (  # noqa: F401
     PowerAttnError,
     library_path,
     load_library,
+    make_cache,
     power_attn_bwd,
+    power_attn_cache_append,
+    power_attn_cache_bytes,
+    power_attn_cache_read,
+    power_attn_cache_step,
+    power_attn_cache_step_workspace_bytes,
+    power_attn_exp_bwd,
+    power_attn_exp_fwd,
     power_attn_fwd,
     power_attn_workspace_bytes,
 )

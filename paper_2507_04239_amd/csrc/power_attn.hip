@@ -460,6 +460,10 @@ pa_status power_attn_decode_step(const pa_problem* prob, const void* q, const vo
 // ---- exponential attention and its cache ----
 static bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
+// A capped score is formed from a value that is rounded at the size of the cap: off by up to 2e-7 of it, which beyond this would be more
+// than the weights' rounding to bf16.
+constexpr float MOST_CAP = 1e4f;
+
 // score and window of pa_exp_problem and pa_cache; with a cap 2 scale / cap is a factor of its own, in units of log 2
 static bool score_ok(float scale, float cap, int window) {
     if (!std::isfinite(scale) || !(scale > 0.f) || !std::isfinite(cap) || !(cap >= 0.f) || window < 0) return false;
@@ -472,7 +476,7 @@ static pa_status validate_exp(const pa_exp_problem* pr) {
     if (!score_ok(pr->scale, pr->cap, pr->window)) return PA_ERR_INVALID_ARG;
     if (pr->dtype != PA_DTYPE_F32 && pr->dtype != PA_DTYPE_BF16) return PA_ERR_INVALID_ARG;
     if (pr->dtype != PA_DTYPE_BF16 || (pr->d != 32 && pr->d != 64 && pr->d != 128)) return PA_ERR_UNSUPPORTED;
-    if (pr->T > (1 << 30) || pr->Tk > (1 << 30) || (long long)pr->B * pr->H > 0x7fffffffLL || !exp_grid_ok(*pr)) return PA_ERR_UNSUPPORTED;
+    if (pr->cap > MOST_CAP || pr->T > (1 << 30) || pr->Tk > (1 << 30) || (long long)pr->B * pr->H > 0x7fffffffLL || !exp_grid_ok(*pr)) return PA_ERR_UNSUPPORTED;
     return PA_OK;
 }
 
@@ -531,7 +535,7 @@ static pa_status validate_cache(const pa_cache* c) {
     if (!score_ok(c->scale, c->cap, c->window)) return PA_ERR_INVALID_ARG;
     const long long positions = (long long)c->max_pages * c->page;
     if (c->rot > 0 && c->rot_rows < positions) return PA_ERR_INVALID_ARG;
-    if ((c->d != 64 && c->d != 128) || positions > (1 << 30) || c->B > 65535 || c->H + c->Hk > 65535 ||
+    if ((c->d != 64 && c->d != 128) || c->cap > MOST_CAP || positions > (1 << 30) || c->B > 65535 || c->H + c->Hk > 65535 ||
         (long long)c->B * c->H > (1 << 30) || c->B * positions >= (1LL << 36))
         return PA_ERR_UNSUPPORTED;
     return PA_OK;

@@ -23,7 +23,7 @@ OK = dict(B=1, H=4, Hk=2, T=10, Tk=20, d=64, scale=1.0, cap=0.0, window=0, dtype
     (1, dict(B=0)), (1, dict(H=0)), (1, dict(Hk=0)), (1, dict(T=0)), (1, dict(Tk=-1)), (1, dict(d=0)), (1, dict(H=5)), (1, dict(Hk=8)),
     (1, dict(scale=0.0)), (1, dict(scale=-1.0)), (1, dict(scale=math.nan)), (1, dict(scale=math.inf)), (1, dict(cap=-1.0)),
     (1, dict(cap=math.nan)), (1, dict(cap=math.inf)), (1, dict(cap=1e-40)), (1, dict(window=-1)), (2, dict(d=48)), (2, dict(d=256)),
-    (2, dict(dtype="f32")), (2, dict(T=2 ** 30 + 1)), (2, dict(Tk=2 ** 31 - 1)), (2, dict(B=2 ** 20, H=2 ** 12, Hk=2 ** 12)),
+    (2, dict(dtype="f32")), (2, dict(cap=10001.0)), (2, dict(T=2 ** 30 + 1)), (2, dict(Tk=2 ** 31 - 1)), (2, dict(B=2 ** 20, H=2 ** 12, Hk=2 ** 12)),
     (2, dict(B=2 ** 15, T=2 ** 28)),
 ])
 def test_problems(lib, status, change):
@@ -62,7 +62,7 @@ CACHE = dict(B=2, H=4, Hk=2, d=64, page=64, max_pages=4, num_pages=9, bits=4, ro
     (1, dict(B=0)), (1, dict(H=3)), (1, dict(Hk=0)), (1, dict(d=-1)), (1, dict(page=0)), (1, dict(page=16)), (1, dict(page=96)),
     (1, dict(page=2048)), (1, dict(max_pages=0)), (1, dict(num_pages=0)), (1, dict(bits=8)), (1, dict(rot=8)), (1, dict(rot=-16)),
     (1, dict(rot=80)), (1, dict(rot_rows=255)), (1, dict(scale=0.0)), (1, dict(cap=-1.0)), (1, dict(window=-1)), (2, dict(d=32)),
-    (2, dict(d=256)), (2, dict(max_pages=2 ** 25, rot=0)), (2, dict(B=65536)), (2, dict(H=65535, Hk=1)),
+    (2, dict(d=256)), (2, dict(cap=2e4)), (2, dict(max_pages=2 ** 25, rot=0)), (2, dict(B=65536)), (2, dict(H=65535, Hk=1)),
 ])
 def test_caches(lib, status, change):
     c = pa.make_cache(**{**CACHE, **change})
