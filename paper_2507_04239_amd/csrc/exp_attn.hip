@@ -264,6 +264,9 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
     // In log 2 units the score is s = factor x + offset, with x what is compared and masked: the product itself, or minus the r of a
     // capped one; with a bias the score.
     const float factor = BIAS ? 1.f : CAP ? 2.f * sc.capl : sc.sl, offset = CAP && !BIAS ? sc.capl : 0.f;
+    // A capped score is at most the cap: where the least one still gives a normal float32 weight against it (2 cap log2 e <= 100), the
+    // cap is the reference and no maximum is looked for (T1024 of Tk8192, H16/4, d128: 98 us with, 93 without).
+    const bool fixed = CAP && !BIAS && sc.capl <= 50.f;
     const Reads<HD> rd(lane);
     auto tile = [&](int buf, int key0) {
         const uint32_t kt = lds_address(sm.k[0].at) + buf * Tile<HD>::BYTES, vt = kt + 2 * Tile<HD>::BYTES;
@@ -299,23 +302,25 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
                 for (int i = 0; i < 16; ++i)
                     if ((unsigned)(key + 32 * kb + 8 * (i >> 2) + (i & 3)) >= (unsigned)n) c[kb][i] = NEG_INF;
         }
-        float top[2] = {NEG_INF, NEG_INF};
+        if (!fixed) {
+            float top[2] = {NEG_INF, NEG_INF};
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top[kb] = fmaxf(top[kb], c[kb][i]);
-        float lo, hi;
-        halves(fmaxf(top[0], top[1]), lo, hi);
-        const float t = fmaf(fmaxf(lo, hi), factor, offset);
-        if (__any(t > m + 8.f)) {
-            const float to = fmaxf(t, m);
-            const float f = to == NEG_INF ? 1.f : __builtin_amdgcn_exp2f(m - to);
-            m = to;
-            lsum *= f;
+                for (int i = 0; i < 16; ++i) top[kb] = fmaxf(top[kb], c[kb][i]);
+            float lo, hi;
+            halves(fmaxf(top[0], top[1]), lo, hi);
+            const float t = fmaf(fmaxf(lo, hi), factor, offset);
+            if (__any(t > m + 8.f)) {
+                const float to = fmaxf(t, m);
+                const float f = to == NEG_INF ? 1.f : __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                lsum *= f;
 #pragma unroll
-            for (int vb = 0; vb < NV; ++vb)
+                for (int vb = 0; vb < NV; ++vb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[vb][i] *= f;
+                    for (int i = 0; i < 16; ++i) acc[vb][i] *= f;
+            }
         }
         const float by = offset - (m == NEG_INF ? 0.f : m);
 #pragma unroll
@@ -339,7 +344,7 @@ __global__ __launch_bounds__(256, WPE) void k_exp_fwd(const bf16_t* __restrict__
 #pragma unroll
         for (int vb = 0; vb < NV; ++vb) acc[vb] = splat16(0.f);
         lsum = 0.f;
-        m = NEG_INF;
+        m = fixed ? sc.capl : NEG_INF;
         if (t_lo < t_hi) {
             tile_load(sm.k[0], Kh, t_lo * AT, T, lane, w);
             tile_load(sm.v[0], Vh, t_lo * AT, T, lane, w);
