@@ -89,16 +89,17 @@ __device__ __forceinline__ Ends wave_ends(Range r) {
 
 // ---- the streamed tile ------------------------------------------------------------------------------------
 // 64 rows, moved from memory to LDS without a register on the way: 16 bytes a lane, so 1 KB of a wave's rows lies one behind the
-// other in LDS.  Two things keep the rows that one cycle of a read touches on different banks: each such KB starts 16 bytes further,
-// and inside it a row's 16-byte pieces are permuted by the row's number.  The permutation leaves enough address bits alone
-// that all of a lane's reads are a few addresses, formed once, and constants.
+// other in LDS.  The rows that one cycle of a read touches (of 16 bytes: lanes 0 - 3, 12 - 15, 20 - 23, 24 - 27 and the like; transposing: 4
+// rows of 64 bytes) are kept on different banks by a permutation of a row's 16-byte pieces by the row's number, and with 128 channels by 16 bytes
+// more from one such KB to the next.  Either leaves enough address bits alone that all of a lane's reads are a few addresses, formed
+// once, and constants.
 template <int HD>
 struct Tile {
-    static constexpr int PIECES = HD / 8, RUN = 512 / HD, STEP = 1040, BYTES = AT / RUN * STEP;     // rows of a KB; their distance
-    static constexpr int NROW = HD == 32 ? 2 : 4, NCOL = HD == 128 ? 4 : 2;
+    static constexpr int PIECES = HD / 8, RUN = 512 / HD, STEP = HD == 128 ? 1040 : 1024, BYTES = AT / RUN * STEP;     // rows of a KB; their distance
+    static constexpr int NROW = HD == 32 ? 2 : 4, NCOL = HD / 32, HALVES = HD == 128 ? 1 : 2;
     uint4 at[BYTES / 16];
     static __device__ __forceinline__ int turn(int row) {
-        return HD == 128 ? (row & 3) << 2 : HD == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 1) << 1 : (row >> 2 & 1) << 1 | (row >> 3 & 1);
+        return HD == 128 ? (row & 3) << 2 : HD == 64 ? (row >> 1 & 1) << 2 | (row >> 2 & 1) << 1 | (row >> 3 & 1) : (row >> 2 & 1) << 1 | (row >> 3 & 1);
     }
     // byte of piece `piece` of a row
     static __device__ __forceinline__ uint32_t place(int row, int piece) {
@@ -113,10 +114,10 @@ __device__ __forceinline__ void tile_load(const Tile<HD>& t, const bf16_t* __res
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(t.at));
     const uint64_t tile0 = uniform64((uint64_t)(head + (size_t)row0 * HD));
     const int last = T - 1 - row0, row = lane / TL::PIECES;
-    const uint32_t piece = (uint32_t)(lane % TL::PIECES ^ TL::turn(row)) * 16;      // (turn() is the same in every KB)
 #pragma unroll
     for (int q = 0; q < HD / 32; ++q) {
         const int run = 4 * q + w;
+        const uint32_t piece = (uint32_t)(lane % TL::PIECES ^ TL::turn(run * TL::RUN + row)) * 16;
         const uint32_t off = (uint32_t)min(run * TL::RUN + row, last) * (2 * HD) + piece;
         dma16(tile0, off, base + run * TL::STEP);
     }
@@ -125,14 +126,16 @@ __device__ __forceinline__ void tile_load(const Tile<HD>& t, const bf16_t* __res
 // A lane's addresses in a tile
 template <int HD>
 struct Reads {
-    uint32_t row[Tile<HD>::NROW], col[Tile<HD>::NCOL];
+    uint32_t row[Tile<HD>::NROW], col[Tile<HD>::HALVES][Tile<HD>::NCOL];
     __device__ __forceinline__ explicit Reads(int lane) {
         const int r16 = lane & 15, h = lane >> 5, odd = lane >> 4 & 1;
 #pragma unroll
         for (int x = 0; x < Tile<HD>::NROW; ++x) row[x] = Tile<HD>::place(lane & 31, (HD == 128 ? 4 : 2) * x + h);
 #pragma unroll
-        for (int x = 0; x < Tile<HD>::NCOL; ++x)
-            col[x] = Tile<HD>::place(4 * h + (r16 >> 2) + (HD == 32 ? 8 * x : 0), (HD == 32 ? 0 : 4 * x) + 2 * odd + (r16 >> 1 & 1)) + 8 * (r16 & 1);
+        for (int e = 0; e < Tile<HD>::HALVES; ++e)
+#pragma unroll
+            for (int x = 0; x < Tile<HD>::NCOL; ++x)
+                col[e][x] = Tile<HD>::place(8 * e + 4 * h + (r16 >> 2), 4 * x + 2 * odd + (r16 >> 1 & 1)) + 8 * (r16 & 1);
     }
 };
 // rows 32 blk + r32, features 16 ks + 8 h .. + 7 (A or B operand of a contraction over the features); tile: its address
@@ -147,8 +150,8 @@ __device__ __forceinline__ bf16x8 row_op(uint32_t tile, const Reads<HD>& rd, int
 template <int HD>
 __device__ __forceinline__ bf16x8 col_op(uint32_t tile, const Reads<HD>& rd, int j, int cb) {
     constexpr int STEP = Tile<HD>::STEP, RUN = Tile<HD>::RUN;
-    const uint32_t at = tile + rd.col[HD == 32 ? 0 : cb] + j * (16 / RUN * STEP);
-    const uint32_t at8 = HD == 32 ? tile + rd.col[1] + j * STEP : at + 8 / RUN * STEP;
+    const uint32_t at = tile + rd.col[0][cb] + j * (16 * STEP / RUN);
+    const uint32_t at8 = HD == 128 ? at + 8 / RUN * STEP : tile + rd.col[Tile<HD>::HALVES - 1][cb] + j * (16 * STEP / RUN);
     union {
         bf16x8 v;
         bf16x4 h[2];
