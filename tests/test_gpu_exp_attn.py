@@ -53,6 +53,37 @@ def test_lengths(d, T):
     both(q, k, v, g, scale=d ** -0.5)
 
 
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("T", [2, 4, 6, 16, 40])
+@pytest.mark.parametrize("cap", [0.0, 15.0])
+def test_gradients_of_rows_of_few_keys(d, T, cap):
+    """dO . v_j and their mean under the weights cancel; what is left is off by two roundings to bf16, of the scores' gradients and of the
+    results, each by 2^-8 at most and independent of the other."""
+    q, k, v, g = make(60, 6, 2, T, T, d, seed=T, sharp=4.0)
+    how = dict(scale=d ** -0.5, cap=cap)
+    got, want = run(q, k, v, g, **how), exp_attn(q, k, v, g=g, **how)
+    for n in ("dQ", "dK"):
+        off = float((got[n].double() - want[n]).norm() / want[n].norm())
+        print(d, T, cap, n, off, flush=True)
+        assert off <= 2 ** -8 * math.sqrt(2)
+
+
+@pytest.mark.parametrize("cap", [0.0, 15.0])
+def test_scores_of_rows_of_one_key_have_no_gradient(cap):
+    for T, Tk, how in ((1, 1, {}), (5, 1, {}), (150, 150, {"window": 1})):
+        q, k, v, g = make(2, 4, 2, T, Tk, 64, seed=T, sharp=4.0)
+        got = run(q, k, v, g, scale=0.125, cap=cap, **how)
+        assert not got["dQ"].any() and not got["dK"].any() and got["dV"].any()
+
+
+def test_window_of_one_key_before_a_prefix():
+    """Rows that see keys behind themselves: a window counts back from the row only."""
+    T = 100
+    hi = torch.arange(1, T + 1, dtype=torch.int32).clamp(min=30)[None]
+    q, k, v, g = make(1, 2, 1, T, T, 64, seed=4)
+    both(q, k, v, g, scale=0.125, window=1, lo=torch.zeros(1, T, dtype=torch.int32), hi=hi)
+
+
 @pytest.mark.parametrize("H,Hk", [(4, 1), (6, 2), (8, 8), (3, 3), (9, 3)])
 def test_heads_that_share_a_key_head(H, Hk):
     q, k, v, g = make(2, H, Hk, 150, 150, 64, seed=H)
