@@ -286,7 +286,7 @@ pa_status power_attn_cache_read(const pa_cache* cache, int T, const void* pool, 
                                 const int* count, void* K, void* V, void* hip_stream);
 /* One token for every sequence: q [B, H, d] (rotated), the last of lens[b] tokens held, attends to them (pos = lens[b] - 1):
  * o [B, H, d] and, where L is not NULL, L [B, H] as power_attn_exp_fwd has them.  lens[b] <= 0: o = 0, L = -infinity; lengths are
- * limited to the table.  4 bits: the values enter the products as fp16.  workspace: DEVICE, 256-byte aligned. */
+ * limited to the table.  4 bits: the values' x enter their product as fp16.  workspace: DEVICE, 256-byte aligned. */
 size_t power_attn_cache_step_workspace_bytes(const pa_cache* cache);
 pa_status power_attn_cache_step(const pa_cache* cache, const void* q, const float* slopes, const void* pool, const int* table,
                                 const int* lens, void* o, float* L, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -501,27 +501,61 @@ union Half8 {
     f16x8 v;
     f16x2 h[4];
 };
+// Scores of 16 held keys.  q . k = sum over groups of u (q . c) + m sum q, which leaves no rounding of u c + m in them (in fp16, 2^-11 of an element: the
+// largest error in L, 6e-5 of it at 300 tokens and scores of standard deviation 4): codes and q are exact operands, the units multiply in
+// float32, and the minima are one more product, with the groups' sums of q in three fp16 parts (sums_op).
 template <int HD>
-__device__ __forceinline__ void key_ops4(f16x8 (&op)[HD / 32], uint32_t lds, int blk, int lane, uint32_t magic) {
+__device__ __forceinline__ f32x4 key_scores4(uint32_t lds, int blk, int lane, uint32_t magic, const f16x8 (&qf)[HD / 32], f16x8 q_sums) {
     constexpr int NK = HD / 32;
     typedef __attribute__((ext_vector_type(NK))) uint32_t words;
+    typedef __attribute__((ext_vector_type(NK / 2))) uint32_t half_words;
     using LP = __attribute__((address_space(3))) const words*;
+    using LH = __attribute__((address_space(3))) const half_words*;
     const words w = *(LP)(uintptr_t)(lds + blk * (Unit<HD, 4>::CODES / 2) + lane * (HD / 8));
+    const uint32_t par = lds + 2 * Unit<HD, 4>::CODES + 16 * blk * (HD / 8);        // of a key: NK units, NK minima
     union {
-        words u;
-        _Float16 h[2 * NK];
-    } par;
-    par.u = *(LP)(uintptr_t)(lds + 2 * Unit<HD, 4>::CODES + (16 * blk + lane % 16) * (HD / 8));
+        half_words u;
+        _Float16 h[NK];
+    } unit[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) unit[r].u = *(LH)(uintptr_t)(par + (4 * (lane >> 4) + r) * (HD / 8));
+    union {
+        half_words u[8 / NK];
+        f16x8 v;
+    } least{};
+    least.u[0] = *(LH)(uintptr_t)(par + lane % 16 * (HD / 8) + HD / 16);
+    f32x4 s = mfma_step(least.v, q_sums, (f32x4){0.f, 0.f, 0.f, 0.f});
 #pragma unroll
     for (int ks = 0; ks < NK; ++ks) {
-        const f16x2 u = {par.h[ks], par.h[ks]}, m = {par.h[NK + ks], par.h[NK + ks]};
         Half8 o;
-        o.h[0] = __builtin_elementwise_fma(codes2<0>(w[ks], magic), u, m);
-        o.h[1] = __builtin_elementwise_fma(codes2<4>(w[ks], magic), u, m);
-        o.h[2] = __builtin_elementwise_fma(codes2<8>(w[ks], magic), u, m);
-        o.h[3] = __builtin_elementwise_fma(codes2<12>(w[ks], magic), u, m);
-        op[ks] = o.v;
+        o.h[0] = codes2<0>(w[ks], magic);
+        o.h[1] = codes2<4>(w[ks], magic);
+        o.h[2] = codes2<8>(w[ks], magic);
+        o.h[3] = codes2<12>(w[ks], magic);
+        const f32x4 c = mfma_step(o.v, qf[ks], (f32x4){0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = fmaf((float)unit[r].h[ks], c[r], s[r]);
     }
+    return s;
+}
+// column of this lane: slot ks of lane group n = part n of the sum of q's group ks (parts of 11 bits: all of a float32)
+template <int NK>
+__device__ __forceinline__ f16x8 sums_op(const f16x8 (&qf)[NK], int lane) {
+    f16x8 op = {};
+#pragma unroll
+    for (int ks = 0; ks < NK; ++ks) {
+        float x = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x += (float)qf[ks][e];
+        x += __shfl_xor(x, 16);
+        x += __shfl_xor(x, 32);
+        for (int n = 0; n < 3; ++n) {
+            const _Float16 part = (_Float16)x;
+            if (lane >> 4 == n) op[ks] = part;
+            x -= (float)part;
+        }
+    }
+    return op;
 }
 // channels 32 cg .. + 31: two operands
 template <int HD>
@@ -584,7 +618,7 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     auto piece = [&](int b, Visible vis, int u, int u_end, bool whole) {
         // the head of this lane's column
         const int hq = 16 * mb + r16, head = hk * G + min(hq, G - 1);
-        vec qf[NK];
+        vec qf[NK], q_sums = {};
         float factor = 1.f;
         {
             Frag raw[NK];
@@ -610,6 +644,7 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
                 for (int ks = 0; ks < NK; ++ks)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) qf[ks][e] = (_Float16)((float)raw[ks].v[e] * inv);
+                q_sums = sums_op(qf, lane);
             }
         }
         const float slope = BIAS ? slopes[head] * 1.44269504088896340736f : 0.f;
@@ -626,15 +661,12 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
             f32x4 s[2];
 #pragma unroll
             for (int blk = 0; blk < 2; ++blk) {
-                s[blk] = (f32x4){0.f, 0.f, 0.f, 0.f};
                 if constexpr (BITS == 16) {
+                    s[blk] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(key_op<HD>(bits, at_lds, blk, ks, lane, magic), qf[ks], s[blk]);
                 } else {
-                    vec kop[NK];
-                    key_ops4<HD>(kop, at_lds, blk, lane, magic);
-#pragma unroll
-                    for (int ks = 0; ks < NK; ++ks) s[blk] = mfma_step(kop[ks], qf[ks], s[blk]);
+                    s[blk] = key_scores4<HD>(at_lds, blk, lane, magic, qf, q_sums);
                 }
             }
             const float far = BIAS ? (float)(vis.len - 1 - tok0) : 0.f;

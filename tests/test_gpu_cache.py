@@ -369,3 +369,21 @@ def test_pools_beyond_32_bits(bits, page_bytes):
     o, L = pa.power_attn_cache_step(c, q.to(DEV), pool, table, small.ints([1100]))
     want = small.step(q, [1100])
     assert torch.equal(o.float().cpu(), want[0]) and torch.equal(L.cpu(), want[1])
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_log_sums_are_float32(bits, d, cap):
+    """L of the values as they are held: a score is a sum of d products and d / 32 more in float32, whose roundings (2^-24 of a term each)
+    add up as squares: about 2^-24 sqrt(d) of sqrt(sum of the terms' squares), for scores of standard deviation 4 not over 2e-6 of L."""
+    c = Cache(12, 4, 2, d, 32, 10, bits, scale=d ** -0.5, cap=cap)
+    lens = [298, 1, 2, 31, 64, 100, 150, 200, 250, 320, 7, 299]
+    c.fill(lens, seed=d)
+    q, slopes = queries(12, 4, d, sharp=4.0), torch.tensor([0.3, 0.07, 0.01, 0.0])
+    _, L = c.step(q, lens, slopes)
+    want = torch.stack([exp_attn(q[b:b + 1, :, None], c.k[b:b + 1, :, :n], c.v[b:b + 1, :, :n], slopes=slopes, **c.score)["L"][0, :, 0]
+                        for b, n in enumerate(lens)])
+    off = float((L.double() - want).norm() / want.norm())
+    print(bits, d, cap, off, flush=True)
+    assert off <= 4e-6
