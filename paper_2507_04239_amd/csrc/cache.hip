@@ -130,7 +130,10 @@ __device__ __forceinline__ void hold8(Held& to, const float (&x)[8]) {
     hi = fmaxf(hi, quad<0xB1>(hi));
     lo = least(lo, quad<0x4E>(lo));
     hi = fmaxf(hi, quad<0x4E>(hi));
-    to.unit = (float)(_Float16)((hi - lo) * (1.f / 15.f));
+    // (the product is a float32 before it is an fp16: one instruction could do both, and would round ties by what the float32 has lost)
+    float unit = (hi - lo) * (1.f / 15.f);
+    asm("" : "+v"(unit));
+    to.unit = (float)(_Float16)unit;
     to.least = (float)(_Float16)lo;
     // The quotient by way of a reciprocal is off by a few 2^-24 of it, which matters only next to the middle between two codes: there the
     // division itself decides (four prompts of up to 3000 tokens, 4 key heads of 128: 23.1 us with divisions alone, 21.5).

@@ -387,3 +387,26 @@ def test_log_sums_are_float32(bits, d, cap):
     off = float((L.double() - want).norm() / want.norm())
     print(bits, d, cap, off, flush=True)
     assert off <= 4e-6
+
+
+@pytest.mark.parametrize("rot", [0, 64])
+def test_units_are_rounded_from_float32(rot):
+    """Groups whose (max - min) (1 / 15), rounded to float32, lies in the middle between two fp16 numbers, with what was rounded off on either side."""
+    gen = torch.Generator().manual_seed(7)
+    x = (torch.randn(1 << 22, 2, generator=gen) * 3).bfloat16().float()
+    u = (x[:, 0] - x[:, 1]).abs() * torch.full((1 << 22,), 1.0 / 15.0)
+    tie = ((u.double() - u.half().double()).abs() == (torch.ldexp(torch.ones(1), torch.frexp(u)[1] - 12).double())).nonzero()[:, 0]
+    n = min(int(tie.numel()), 128)
+    print(n, flush=True)
+    assert n == 128
+    c = Cache(1, 1, 1, 64, 32, 2, 4, rot=rot)
+    if rot:     # no turn, in as many operations
+        c.cos, c.sin = torch.ones_like(c.cos).to(c.cos), torch.zeros_like(c.sin)
+    K = torch.rand(1, 1, 64, 2, 32, generator=gen)
+    low, high = (f(x[tie[:n]], -1).values.view(64, 2, 1) for f in (torch.min, torch.max))
+    K = (low + (high - low) * K).bfloat16().clamp(min=low.bfloat16(), max=high.bfloat16())
+    K[0, 0, :, :, :1], K[0, 0, :, :, 1:2] = low.bfloat16(), high.bfloat16()
+    K = K.view(1, 1, 64, 64)
+    c.append(K, K.flip(2), [0])
+    k, v = c.read([0], 64)
+    assert torch.equal(k, c.k.bfloat16().float()) and torch.equal(v, c.v.bfloat16().float())
