@@ -222,7 +222,8 @@ pa_status power_attn_decode_step(const pa_problem* prob, const void* q, const vo
  * and passes no gradient.  What the rows and keys that a row does not see hold, infinities and NaN among it, does not reach it.
  * bf16, d in {32, 64, 128}, T and Tk up to 2^30 tokens.  Q, O, dO, dQ [B, H, T, d], K, V, dK, dV [B, Hk, Tk, d], L float32
  * [B, H, T], slopes float32 [H], not differentiated.  Pointers, streams, threads and errors as for the calls above, but that
- * L, slopes, lo and hi need the alignment of their type only.  Results do not change from run to run. */
+ * L, slopes, lo and hi need the alignment of their type only.  No output may overlap another tensor of the call.  Results do not change
+ * from run to run. */
 typedef struct {
     int   B, H, Hk;     /* batch, query heads, key heads (H a multiple of Hk) */
     int   T, Tk, d;     /* queries, keys, head size */

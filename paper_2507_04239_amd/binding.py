@@ -431,8 +431,17 @@ def power_attn_decode_step(prob: PaProblem, q, k, v, state, log_g=None, out=None
 
 
 # ---- exponential attention ----
+def _c_ints(*values):
+    """The values as they are, which ctypes would cut to 32 bits without a word"""
+    values = [operator.index(x) for x in values]
+    if not all(-2 ** 31 <= x < 2 ** 31 for x in values):
+        raise PowerAttnError(f"sizes must fit 32 bits: {values}")
+    return values
+
+
 def make_exp_problem(B, H, Hk, T, Tk, d, scale=1.0, cap=0.0, window=0, dtype="bf16") -> PaExpProblem:
-    return PaExpProblem(B, H, Hk, T, Tk, d, float(scale), float(cap), int(window), PA_DTYPE_BF16 if dtype == "bf16" else PA_DTYPE_F32)
+    *sizes, window = _c_ints(B, H, Hk, T, Tk, d, window)
+    return PaExpProblem(*sizes, float(scale), float(cap), window, PA_DTYPE_BF16 if dtype == "bf16" else PA_DTYPE_F32)
 
 
 @functools.lru_cache(maxsize=512)
@@ -453,6 +462,13 @@ def _tensor_ptr(t, index, dtype, shape, name):
 
 def _optional_ptr(t, index, dtype, shape, name):
     return None if t is None else _tensor_ptr(t, index, dtype, shape, name)
+
+
+def _workspace_on(index, need, workspace, device):
+    """_workspace, where one that is given must lie on GPU `index` as one piece"""
+    if workspace is not None and (workspace.get_device() != index or not workspace.is_contiguous()):
+        raise PowerAttnError(f"workspace must be contiguous and on the GPU of the tensors, not on {workspace.device}")
+    return _workspace(need, workspace, device)
 
 
 def _launch(fn, index, what, *args):
@@ -510,7 +526,7 @@ def power_attn_exp_fwd(Q, K, V, scale: float = 1.0, cap: float = 0.0, window: in
     l = L.data_ptr() if out_lse is None else _tensor_ptr(L, index, torch.float32, Q.shape[:3], "L")
     ws = None
     if need > 0:
-        workspace, ws = _workspace(need, workspace, Q.device)
+        workspace, ws = _workspace_on(index, need, workspace, Q.device)
     _launch(load_library().power_attn_exp_fwd, index, "power_attn_exp_fwd", prob, *qkv, *masks, o, l, ws, need)
     return O, L
 
@@ -525,7 +541,7 @@ def power_attn_exp_bwd(Q, K, V, O, L, dO, scale: float = 1.0, cap: float = 0.0, 
     dQ, dK, dV = (torch.empty_like(x) for x in (Q, K, V)) if out is None else out
     grads = (_tensor_ptr(dQ, index, dtype, Q.shape, "dQ"), _tensor_ptr(dK, index, dtype, K.shape, "dK"),
              _tensor_ptr(dV, index, dtype, K.shape, "dV"))
-    workspace, ws = _workspace(need, workspace, Q.device)
+    workspace, ws = _workspace_on(index, need, workspace, Q.device)
     _launch(load_library().power_attn_exp_bwd, index, "power_attn_exp_bwd", prob, *qkv, *masks, *rest, *grads, ws, need)
     return dQ, dK, dV
 
@@ -533,7 +549,8 @@ def power_attn_exp_bwd(Q, K, V, O, L, dO, scale: float = 1.0, cap: float = 0.0, 
 # ---- the paged cache that it decodes from ----
 def make_cache(B, H, Hk, d, page, max_pages, num_pages, bits=16, rot=0, rot_adjacent=False, rot_rows=0, scale=1.0, cap=0.0,
                window=0) -> PaCache:
-    return PaCache(B, H, Hk, d, page, max_pages, num_pages, bits, rot, int(bool(rot_adjacent)), rot_rows, float(scale), float(cap), int(window))
+    *sizes, rot_rows, window = _c_ints(B, H, Hk, d, page, max_pages, num_pages, bits, rot, bool(rot_adjacent), rot_rows, window)
+    return PaCache(*sizes, rot_rows, float(scale), float(cap), window)
 
 
 # What the library says about a cache depends on its fields alone (bytes(cache): by their values).
@@ -600,7 +617,8 @@ def power_attn_cache_read(cache: PaCache, pool, table, start, T: int, count=None
     they are in `out`, and undefined without it."""
     import torch
     (ref, B, _, Hk, d, *_), index, p, t = _cache_inputs(cache, pool, table, "power_attn_cache_read")
-    bf16, i32, shape = torch.bfloat16, torch.int32, (B, Hk, operator.index(T), d)
+    T, = _c_ints(T)
+    bf16, i32, shape = torch.bfloat16, torch.int32, (B, Hk, T, d)
     K, V = out if out is not None else (torch.empty(shape, dtype=bf16, device=pool.device) for _ in range(2))
     _launch(load_library().power_attn_cache_read, index, "power_attn_cache_read", ref, T, p, t, _tensor_ptr(start, index, i32, (B,), "start"),
             _optional_ptr(count, index, i32, (B,), "count"), _tensor_ptr(K, index, bf16, shape, "K"), _tensor_ptr(V, index, bf16, shape, "V"))
@@ -615,7 +633,7 @@ def power_attn_cache_step(cache: PaCache, q, pool, table, lens, slopes=None, out
     qp = _tensor_ptr(q, index, bf16, (B, H, d), "q")
     o = torch.empty_like(q) if out is None else out
     L = q.new_empty((B, H), dtype=f32) if out_lse is None else out_lse
-    workspace, ws = _workspace(need, workspace, pool.device)
+    workspace, ws = _workspace_on(index, need, workspace, pool.device)
     _launch(load_library().power_attn_cache_step, index, "power_attn_cache_step", ref, qp, _optional_ptr(slopes, index, f32, (H,), "slopes"),
             p, t, _tensor_ptr(lens, index, torch.int32, (B,), "lens"), o.data_ptr() if out is None else _tensor_ptr(o, index, bf16, (B, H, d), "o"),
             L.data_ptr() if out_lse is None else _tensor_ptr(L, index, f32, (B, H), "L"), ws, need)

@@ -2,8 +2,8 @@
 // attention for every sequence.
 //
 // A page holds, per key head, keys and values in the order in which the matrix instructions of a step (v_mfma_f32_16x16x32) want
-// them as their A operand, so a step's loads go from memory to the operand's registers, 16 bytes a lane and 1 KB of consecutive
-// memory a wave, with nothing transposed on the way.  With lane l = 16 g + r of that operand (row r, k-slots 8 g .. 8 g + 7):
+// them as their A operand, so what a step reads goes from memory to LDS in runs of 1 KB, as it lies, and from there to the operand's
+// registers 16 bytes a lane, with nothing transposed on the way.  With lane l = 16 g + r of that operand (row r, k-slots 8 g .. 8 g + 7):
 //   keys, S^T = K Q^T: rows are 16 tokens, k-slots 32 channels.   16 bits: [token / 16][channel / 32][l] of 16 bytes
 //   values, O^T = V^T P^T: rows are 16 channels, k-slots the 32 tokens of a unit, in the order in which the accumulators of the
 //     first product hold them: slot e of lane group g is token 4 g + e % 4 + 16 (e / 4).   16 bits: [unit][channel / 16][l] of 16 bytes
@@ -191,7 +191,9 @@ __device__ __forceinline__ uint32_t slots_of(uint32_t tokens, int g) { return (t
 
 // ---- rows in -------------------------------------------------------------------------------------------------
 // A workgroup takes the tokens of one unit (32 positions of a page) of one head: y < Hk a key head, the others a query head that is
-// only rotated.  Keys go straight to their place, values through LDS, where a unit's 8 slots come together.
+// only rotated.  Keys go straight to their place, values through LDS, where a unit's 8 slots come together.  Bound by memory where rows are
+// many (4 prompts of up to 3000 tokens, 16 query and 4 key heads of 128, 4 bits: 20 us), by one trip to it and back where they are few
+// (64 sequences, a token each: 4 us).
 struct Take {
     int b, first;           // sequence; position of the unit's first token
     int t0;                 // row of the call at that position (may be negative)
@@ -393,6 +395,12 @@ __global__ __launch_bounds__(256) void k_cache_read(const char* __restrict__ poo
 // units of all sequences, one behind the other, are dealt to the workgroups of a key head in runs of one length, as many as the chip
 // holds at once.  A run may end inside a sequence and begin another: each piece of a sequence leaves its sums in a slot of its own
 // (workgroup + sequence, which no two pieces share) and a second kernel joins them; a sequence that lies in one run is finished there.
+//
+// Bound by memory: a token of a key head is 4 d bytes (1.25 d with 4 bits) read once for all query heads that share it, and a wave's 16
+// columns are those heads.  Each wave keeps DEPTH units on their way in a ring of its own in LDS, so no wave waits for another.
+// 32 sequences of up to 16384 tokens, 4 key heads of 128: 113 us, 5.5 TB/s; 4 of 131072, 8 heads, 4 bits: 127 us, 5.3 TB/s, with the
+// vector pipe 59 % full of codes.  (Through registers instead of the ring: 121 and 267 us.  A fixed number of pieces for each
+// sequence instead of equal runs: 134 and 131.)
 constexpr int RUN_MIN = 4;              // units: one for each wave
 struct Split {
     int runs;               // workgroups per key head (and block of query heads)

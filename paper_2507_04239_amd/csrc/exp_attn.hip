@@ -3,6 +3,7 @@
 //     x_ij = scale q_i . k_j      s_ij = cap tanh(x_ij / cap) - slope_h |pos_i - j|      pos_i = i + Tk - T
 //     L_i = log sum_j exp s_ij    P_ij = exp(s_ij - L_i)    O_i = sum_j P_ij v_j         over the keys lo_i <= j < hi_i
 //     D_i = dO_i . O_i            t_ij = P_ij (dO_i . v_j - D_i) (1 - tanh^2(x_ij / cap))
+//     (D_i is sum_j P_ij dO_i . v_j: how it is formed, k_exp_few)
 //     dQ_i = scale sum_j t_ij k_j     dK_j = scale sum_i t_ij q_i     dV_j = sum_i P_ij dO_i
 // The last two sum over the query heads that share the key head too.
 //
@@ -11,7 +12,15 @@
 // is an interval of keys per query row; blocks of rows know the least and greatest ends of their intervals, so a tile that
 // no row sees is not read, one that every row sees whole has no comparison in it, and only the ones between select.
 //
-// Scores are in units of log 2 from the first multiplication on, so a weight is one multiply-add and one v_exp_f32.
+// Scores are in units of log 2 from the first multiplication on, so a weight is one multiply-add and one v_exp_f32.  Weights and t are
+// rounded to bf16 to be operands, statistics and sums are float32 (the sum of the weights takes them unrounded: L is a float32 result).
+//
+// What bounds them: per pair and pass 4 d (forward), 6 d (dQ) and 8 d (dK, dV) matrix flops stand against one exponential and some ten vector
+// instructions (17 with a cap: a reciprocal and a second exponential), so at d = 128 both pipes are about equally full and at d = 64
+// the vector one is the limit.  B1 H16/8 T16384 d128, causal: forward 1060 us (1.04 PFLOP/s; matrix pipe 56 % of the time, vector
+// pipe 55 %), dQ 1440 us (1.14; 61 %, 41 %), dK and dV 2280 us (0.96; 42 %, 29 %, one wave per SIMD: its registers hold both sums and both
+// operands, and nothing covers its waits).  B4 H12 T8192 d64, window 1024: forward 137 us (vector pipe 81 %).  Short walks
+// (documents of some hundred tokens) pay for their first tiles and their last: B16 H12 T1000 d64 forward 38, dQ 46, dK and dV 65 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -222,7 +231,10 @@ __device__ __forceinline__ bool place(const Order& o, Place& p) {
 // ---- forward --------------------------------------------------------------------------------------------
 // acc[vb][ib] = O^T: value columns 32 vb + .., query 32 ib + r32 of the wave's OWN queries.  One pass: m is the reference of the
 // running sum, in units of log 2; it follows the row's maximum only once that is 8 above it (weights up to 256 lose nothing,
-// and most tiles then rescale nothing).
+// and most tiles then rescale nothing).  Where the scores are capped at 50 or less and have no bias the cap itself is the reference.
+// S^T = K Q^T makes a query a lane, so a tile's statistics need one exchange between the halves of the wave, and the weights are the
+// second product's operand in the registers that they were formed in.  32 queries a wave: with 64 (half the LDS reads a pair) B4 H12 T8192
+// d64, window 1024, takes 184 us, 148 so at the time; 137 now.
 template <int HD>
 struct FwdShared {
     Tile<HD> k[2], v[2];
@@ -446,7 +458,8 @@ __global__ __launch_bounds__(256) void k_exp_fwd_join(const float4* __restrict__
 
 // ---- backward: preparation --------------------------------------------------------------------------------
 // stat[row] = {L log2 e, -dO . O}: what the weights and their gradients are formed from.  A workgroup takes 64 rows of a head, HD / 8 lanes a row;
-// the first head of a batch entry also leaves the rows' intervals and, per 64 rows, their ends.
+// the first head of a batch entry also leaves the rows' intervals and, per 64 rows, their ends.  Bound by memory: B1 H16 T16384 d128,
+// 134 MB in 23 us.
 struct BwdScratch {
     float2* stat;       // [B H][T]
     int2* range;        // [B][T]
@@ -503,7 +516,7 @@ __device__ __forceinline__ void pair_grad(float c, float e, float l2, float slop
 // the result make.  So 64 rows that see few keys between them take D = sum_j P_ij dO_i . v_j from the products instead; rows of many keys
 // average over enough of them (0.4 %).  Two waves take 32 rows and turns at their keys, with both operands straight from memory:
 // what it reads, the other passes are about to.  A workgroup looks at the ends of 64 items, (64 rows, head), at once, one a lane, and goes over
-// those with few keys.
+// those with few keys (B2 H16 T8192 d128, some 500 of 4096 items: 20 us; a workgroup an item 37, most of them only to end).
 constexpr int D_KEYS = 128;     // the 64 rows at the diagonal and a tile before: whole windows up to 65 too
 template <int HD, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) void k_exp_few(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K, const bf16_t* __restrict__ V,
@@ -558,7 +571,9 @@ __global__ __launch_bounds__(256) void k_exp_few(const bf16_t* __restrict__ Q, c
 }
 
 // ---- backward: dQ -------------------------------------------------------------------------------------------
-// acc[fb][ib] = dQ^T / scale: features 32 fb + .., query 32 ib + r32.
+// acc[fb] = dQ^T / scale: features 32 fb + .., query r32.  As the forward pass, with dO V^T - D beside the scores (-D is where its sums begin)
+// and K^T t in the place of V^T P.  A pass of its own, which forms the scores a second time: a third of what both backward walks
+// compute, but nothing is added by atomics and a result has one order.
 template <int HD, int WPE, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ K,
                                                      const bf16_t* __restrict__ V, const float* __restrict__ slopes,
@@ -683,7 +698,8 @@ __global__ __launch_bounds__(256, WPE) void k_exp_dq(const bf16_t* __restrict__ 
 // dk[fb][kb] = dK^T / scale: features 32 fb + .., key 32 kb + r32 of the wave's OWN keys; dv likewise.  The walk goes over the
 // query rows of every head that reads the key head; tiles of rows that see none of the block's keys are found 64 at a time from the
 // ends that the preparation left.  Where there are few blocks, each is walked by several workgroups, which take turns at its tiles;
-// their float32 sums (in the order of the registers) are added by k_exp_dkdv_join.
+// their float32 sums (in the order of the registers) are added by k_exp_dkdv_join.  32 keys a wave in registers, with both sums and both
+// operands: 512 of them at d = 128, so one wave per SIMD (held to 256 it spills 38: T16384 2.42 ms and 3.18).
 template <int HD>
 struct BwdShared {
     Tile<HD> q[2], g[2];
@@ -1054,8 +1070,8 @@ pa_status bwd_t(const pa_exp_problem& pr, const bf16_t* Q, const bf16_t* K, cons
                            ntile);
         if (!launch_ok()) return PA_ERR_HIP;
     }
-    // without documents and with a window that is no short one only the first rows see few keys
-    const bool anywhere = mk.lo != nullptr || (pr.window > 0 && pr.window < D_KEYS);
+    // without intervals and with a window that is no short one only the first rows see few keys
+    const bool anywhere = mk.lo != nullptr || mk.hi != nullptr || (pr.window > 0 && pr.window < D_KEYS);
     const int few = anywhere ? ntile : std::min(ntile, std::max(0, (D_KEYS - (pr.Tk - pr.T) + AT - 1) / AT));
     if (few > 0) {
         const int items = pr.B * pr.H * few;

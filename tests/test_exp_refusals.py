@@ -129,3 +129,20 @@ def test_plans_of_a_cache_follow_its_fields():
     before = pa.power_attn_cache_bytes(c)
     c.num_pages *= 2
     assert pa.power_attn_cache_bytes(c) == 2 * before
+
+
+def test_sizes_beyond_32_bits_are_refused_and_not_cut():
+    for change in (dict(window=2 ** 32 + 5), dict(T=2 ** 32 + 10), dict(B=-2 ** 40)):
+        with pytest.raises(pa.PowerAttnError):
+            pa.make_exp_problem(**{**OK, **change})
+    for change in (dict(num_pages=2 ** 32 + 4), dict(window=2 ** 31), dict(rot_rows=2 ** 33)):
+        with pytest.raises(pa.PowerAttnError):
+            pa.make_cache(**{**dict(B=1, H=4, Hk=2, d=64, page=32, max_pages=4, num_pages=4), **change})
+    assert pa.make_exp_problem(**{**OK, "window": 2 ** 31 - 1}).window == 2 ** 31 - 1
+
+
+def test_workspaces_that_a_kernel_cannot_use():
+    import torch
+    for workspace in (torch.empty(4096, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8).expand(4096)):
+        with pytest.raises(pa.PowerAttnError):
+            pa._workspace_on(0, 1024, workspace, "cuda:0")
