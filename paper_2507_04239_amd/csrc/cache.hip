@@ -403,7 +403,7 @@ __global__ __launch_bounds__(256) void k_cache_read(const char* __restrict__ poo
 // sequence instead of equal runs: 134 and 131.)
 constexpr int RUN_MIN = 4;              // units: one for each wave
 struct Split {
-    int runs;               // workgroups per key head (and block of query heads)
+    int runs;               // workgroups per key head (and block of query heads); 0: one to a sequence, and nothing to join
     int slots;              // runs + B
 };
 struct Visible {
@@ -615,9 +615,21 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     const int mblks = (G + 15) / 16, per = pg.Hk * mblks;
     const int run = (int)(blockIdx.x / (unsigned)per), rest = (int)(blockIdx.x - (unsigned)run * (unsigned)per);
     const int hk = rest / mblks, mb = rest - hk * mblks;
-    const int total = total_units(lens, B, pg, window, lane), C = run_units(total, split.runs);
-    if (run > (total - 1) / C || total == 0) return;
-    const int begin = run * C, end = begin + min(C, total - begin);
+    const bool alone = split.runs == 0;
+    const int b0 = alone ? run : 0, nb = alone ? 1 : B;        // the sequences that are looked at
+    const int total = total_units(lens + b0, nb, pg, window, lane), C = alone ? total : run_units(total, split.runs);
+    if (total == 0) {
+        if (alone) {
+            const int h = tid / 16, hd = hk * G + 16 * mb + h;
+            if (16 * mb + h < G) {
+                for (int c = 8 * (tid % 16); c < HD; c += 128) *(uint4*)(o + ((size_t)b0 * H + hd) * HD + c) = make_uint4(0, 0, 0, 0);
+                if (tid % 16 == 0 && L != nullptr) L[(size_t)b0 * H + hd] = STEP_NONE;
+            }
+        }
+        return;
+    }
+    if (!alone && run > (total - 1) / C) return;
+    const int begin = alone ? 0 : run * C, end = begin + min(C, total - begin);
 
     uint32_t magic;
     asm("v_mov_b32 %0, 0x64006400" : "=v"(magic));
@@ -815,8 +827,8 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
     };
 
     int before = 0;
-    for (int base = 0; base < B && before < end; base += 64) {
-        const Visible v = visible(lens, base + lane, B, pg, window);
+    for (int base = 0; base < nb && before < end; base += 64) {
+        const Visible v = visible(lens + b0, base + lane, nb, pg, window);
         const int upto = before + wave_scan(v.units);
         uint64_t mine = __ballot(v.units > 0 && upto > begin && upto - v.units < end);
         for (; mine != 0; mine &= mine - 1) {
@@ -824,7 +836,7 @@ __global__ __launch_bounds__(256) void k_cache_step(const bf16_t* __restrict__ q
             const Visible vis{__builtin_amdgcn_readlane(v.len, at), __builtin_amdgcn_readlane(v.first, at), __builtin_amdgcn_readlane(v.unit0, at),
                               __builtin_amdgcn_readlane(v.units, at)};
             const int last = __builtin_amdgcn_readlane(upto, at), first = last - vis.units;
-            piece(base + at, vis, vis.unit0 + max(begin - first, 0), vis.unit0 + min(end, last) - first, first >= begin && last <= end);
+            piece(b0 + base + at, vis, vis.unit0 + max(begin - first, 0), vis.unit0 + min(end, last) - first, first >= begin && last <= end);
             __syncthreads();        // the sums have been read: the ring is free
         }
         before = __builtin_amdgcn_readlane(upto, 63);
@@ -887,6 +899,10 @@ Split split_of(const pa_cache& c) {
     const int runs = std::max(8, 256 * resident / per);
     return {runs, runs + c.B};
 }
+// (us in a graph, shared out with the join and one workgroup a sequence: 256 / 500 / 1000 / 2000 tokens, 1 sequence H12 d64 7.9 7.9 8.4 8.9 and
+// 4.8 5.9 7.6 10.9; H32/8 d128 in 4 bits 9.2 9.4 9.7 10.3 and 6.7 8.7 12.4 19.9; 64 sequences of it 11.0 16.5 23.8 35.4 and 9.0 14.0 21.4 33.1,
+// of one length, which a longer table would not promise.)
+constexpr int ALONE = 16;
 size_t part_bytes(const pa_cache& c) { return align_up((size_t)split_of(c).slots * c.H * c.d * sizeof(float), 256); }
 
 template <typename F>
@@ -935,8 +951,13 @@ pa_status cache_read(const pa_cache& c, int T, const void* pool, const int* tabl
 
 pa_status cache_step(const pa_cache& c, const bf16_t* q, const float* slopes, const void* pool, const int* table, const int* lens,
                      bf16_t* o, float* L, char* ws, hipStream_t s) {
-    const Split split = split_of(c);
+    Split split = split_of(c);
     const int G = c.H / c.Hk, window = c.window;
+    // Where no sequence can have more than ALONE units to see, each is one workgroup's, and there is one launch.
+    const long long most = c.window > 0 ? std::min((long long)c.window + UNIT - 1, (long long)c.max_pages * c.page) : (long long)c.max_pages * c.page;
+    const int per = c.Hk * ((G + 15) / 16);
+    const bool alone = (most + UNIT - 1) / UNIT <= ALONE && (long long)c.B * per <= 0x7fffffffLL;
+    if (alone) split.runs = 0;
     const Pages pg = pages_of(c, table);
     float* part = (float*)ws;
     float2* stat = (float2*)(ws + part_bytes(c));
@@ -945,7 +966,7 @@ pa_status cache_step(const pa_cache& c, const bf16_t* q, const float* slopes, co
         sc.kc = (float)(2.0 * c.scale / c.cap * 1.44269504088896340736);
         sc.capl = c.cap * 1.44269504088896340736f;
     }
-    const unsigned grid = (unsigned)split.runs * (unsigned)(c.Hk * ((G + 15) / 16));
+    const unsigned grid = (unsigned)(alone ? c.B : split.runs) * (unsigned)per;
     auto launch = [&](auto hd, auto bits, auto cap, auto bias) {
         LaunchScope ls("cache_step", s);
         hipLaunchKernelGGL((k_cache_step<decltype(hd)::value, decltype(bits)::value, decltype(cap)::value, decltype(bias)::value>), dim3(grid),
@@ -957,7 +978,7 @@ pa_status cache_step(const pa_cache& c, const bf16_t* q, const float* slopes, co
             return slopes != nullptr ? launch(hd, bits, std::true_type{}, std::true_type{}) : launch(hd, bits, std::true_type{}, std::false_type{});
         return slopes != nullptr ? launch(hd, bits, std::false_type{}, std::true_type{}) : launch(hd, bits, std::false_type{}, std::false_type{});
     });
-    if (st != PA_OK) return st;
+    if (st != PA_OK || alone) return st;
     LaunchScope ls("cache_join", s);
     const unsigned rows = (unsigned)(((long long)c.B * c.H + 3) / 4);
     if (c.d == 128)

@@ -410,3 +410,44 @@ def test_units_are_rounded_from_float32(rot):
     c.append(K, K.flip(2), [0])
     k, v = c.read([0], 64)
     assert torch.equal(k, c.k.bfloat16().float()) and torch.equal(v, c.v.bfloat16().float())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("H,Hk,d", [(1, 1, 64), (17, 1, 128), (40, 2, 64), (64, 4, 128)])
+@pytest.mark.parametrize("pages", [6, 40])
+def test_step_of_few_tokens_in_short_and_long_tables(bits, H, Hk, d, pages):
+    """A short table gives each sequence to one workgroup, a long one shares them out; empty sequences and pages that are not there in both."""
+    lens = [130, 0, 1, 77, -3, 192]
+    c = Cache(6, H, Hk, d, 32, pages, bits, scale=d ** -0.5)
+    c.fill(lens)
+    c.check_step(queries(6, H, d), lens)
+    c.table[0, 1], c.table[3, 2], c.table[2, 0] = -1, c.c.num_pages, -7
+    o, L = c.step(queries(6, H, d), lens)
+    for b, there in ((0, [*range(32), *range(64, 130)]), (3, list(range(64))), (5, list(range(192)))):
+        want = exp_attn(queries(6, H, d)[b:b + 1, :, None], c.k[b:b + 1, :, there], c.v[b:b + 1, :, there], hi=torch.tensor([[len(there)]]),
+                        held=2.0 ** -11, **c.score)
+        assert ((o[b].double() - want["O"][0, :, 0]).abs() <= want["eO"][0, :, 0]).all()
+        assert ((L[b].double() - want["L"][0, :, 0]).abs() <= want["eL"][0, :, 0]).all()
+    for b in (1, 2, 4):
+        assert not o[b].any() and (L[b] == -math.inf).all()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_short_tables_in_replays_with_other_lengths(bits):
+    c = Cache(3, 4, 2, 64, 64, 8, bits, scale=0.125, cap=5.0)
+    c.fill([512, 300, 40])
+    q, lens = queries(3, 4, 64).to(DEV), c.ints([1, 1, 1])
+    step = lambda: pa.power_attn_cache_step(c.c, q, c.pool, c.table, lens)
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    for n in ([512, 0, 40], [1, 300, 33], [0, 0, 0], [500, 32, 31]):
+        lens.copy_(c.ints(n))
+        want = [x.clone() for x in step()]
+        for x in out:
+            x.fill_(math.nan)
+        g.replay()
+        assert all(same(x, y) for x, y in zip(want, out)), n
+        c.check_step(q.cpu(), n)
