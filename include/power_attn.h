@@ -258,7 +258,7 @@ pa_status power_attn_exp_bwd(const pa_exp_problem* prob, const void* Q, const vo
  * in the same place.  A page index outside 0 .. num_pages - 1 stands for no page: nothing is written there, reads give zeros,
  * and a step leaves its tokens out.  Two sequences may share pages that are only read.  d in {64, 128}.  Alignment: pool, K, V, Q, q, o, cos, sin 16 bytes, the other
  * arrays that of their type.  Up to 65535 sequences and heads, 2^30 positions a sequence, less than 2^36 in all,
- * and 2^29 rows a call. */
+ * 2^29 rows a call, and num_pages Hk page d up to 2^44. */
 typedef struct {
     int   B, H, Hk, d;              /* sequences, query heads, key heads (H a multiple of Hk), head size */
     int   page;                     /* tokens per page: a power of two, 32 .. 1024 */

@@ -536,7 +536,8 @@ static pa_status validate_cache(const pa_cache* c) {
     const long long positions = (long long)c->max_pages * c->page;
     if (c->rot > 0 && c->rot_rows < positions) return PA_ERR_INVALID_ARG;
     if ((c->d != 64 && c->d != 128) || c->cap > MOST_CAP || positions > (1 << 30) || c->B > 65535 || c->H + c->Hk > 65535 ||
-        (long long)c->B * c->H > (1 << 30) || c->B * positions >= (1LL << 36))
+        (long long)c->B * c->H > (1 << 30) || c->B * positions >= (1LL << 36) ||
+        (double)c->num_pages * c->Hk * c->page * c->d > 0x1p44)      // (a pool whose bytes are far from 64 bits)
         return PA_ERR_UNSUPPORTED;
     return PA_OK;
 }

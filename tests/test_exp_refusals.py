@@ -146,3 +146,10 @@ def test_workspaces_that_a_kernel_cannot_use():
     for workspace in (torch.empty(4096, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8).expand(4096)):
         with pytest.raises(pa.PowerAttnError):
             pa._workspace_on(0, 1024, workspace, "cuda:0")
+
+
+def test_pools_beyond_any_memory(lib):
+    """Their bytes would not fit 64 bits: refused, and not taken for those of a small one."""
+    c = pa.make_cache(**{**CACHE, "H": 32768, "Hk": 32768, "B": 1, "d": 128, "page": 1024, "num_pages": 2 ** 31 - 1, "rot": 0})
+    p = ctypes.c_void_p(4096)
+    assert lib.power_attn_cache_bytes(c) == 0 and lib.power_attn_cache_step(c, p, None, p, p, p, p, None, p, 1 << 40, None) == 2
