@@ -617,7 +617,9 @@ def power_attn_cache_read(cache: PaCache, pool, table, start, T: int, count=None
     they are in `out`, and undefined without it."""
     import torch
     (ref, B, _, Hk, d, *_), index, p, t = _cache_inputs(cache, pool, table, "power_attn_cache_read")
-    T, = _c_ints(T)
+    T = operator.index(T)
+    if not 0 < T < 2 ** 31:
+        raise PowerAttnError(f"power_attn_cache_read: T = {T}")
     bf16, i32, shape = torch.bfloat16, torch.int32, (B, Hk, T, d)
     K, V = out if out is not None else (torch.empty(shape, dtype=bf16, device=pool.device) for _ in range(2))
     _launch(load_library().power_attn_cache_read, index, "power_attn_cache_read", ref, T, p, t, _tensor_ptr(start, index, i32, (B,), "start"),
