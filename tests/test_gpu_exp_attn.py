@@ -273,3 +273,18 @@ def test_offsets_beyond_32_bits():
     assert not dK[:, :, :-200].any() and not dV[:, :, :-200].any()
     got = dict(zip(("O", "L", "dQ", "dK", "dV"), (x.float().cpu() for x in (O, L, dQ, dK[:, :, -200:], dV[:, :, -200:]))))
     check(got, want)
+
+
+def test_very_many_short_sequences():
+    """More blocks of rows than the pass over rows of few keys looks at in one turn; gradients as in test_gradients_of_rows_of_few_keys."""
+    q, k, v, g = make(300, 256, 256, 2, 2, 32, seed=5, sharp=4.0)
+    got = run(q, k, v, g, scale=32 ** -0.5)
+    x = [t.double().requires_grad_() for t in (q, k, v)]
+    s = (x[0].unsqueeze(3) * x[1].unsqueeze(2)).sum(-1) * 32 ** -0.5
+    p = s.masked_fill(torch.ones(2, 2).triu(1).bool(), -math.inf).softmax(-1)
+    ((p.unsqueeze(-1) * x[2].unsqueeze(2)).sum(3) * g.double()).sum().backward()
+    for n, t in zip(("dQ", "dK", "dV"), x):
+        for b in range(0, 300, 50):
+            off = float((got[n].double() - t.grad)[b:b + 50].norm() / t.grad[b:b + 50].norm())
+            print(n, b, off, flush=True)
+            assert off <= 2 ** -8 * math.sqrt(2)
